@@ -50,7 +50,8 @@ typedef enum {
     PD_ERR_WORKSPACE = 4,         /* workspace NULL, misaligned or smaller than pd_workspace_bytes() */
     PD_ERR_CUDA = 5,              /* a CUDA runtime / driver call failed (launch, attribute, tensor map) */
     PD_ERR_BAD_VARIANT = 6,       /* device saw a variant id outside [-1, V) */
-    PD_ERR_DEVICE_TIMEOUT = 7     /* a bounded device-side wait expired */
+    PD_ERR_DEVICE_TIMEOUT = 7,    /* a bounded device-side wait expired */
+    PD_ERR_BAD_INDEX = 8          /* device saw sequence offsets, a length or a page number out of range */
 } pd_status;
 
 typedef enum {
@@ -65,7 +66,8 @@ typedef enum {
     PD_OP_LINEAR_MULTIVARIANT = 2,
     PD_OP_MERGE = 3,
     PD_OP_FIT = 4,       /* pd_fit_loss_grad: M = tokens of the batch */
-    PD_OP_FIT_LAYER = 5  /* pd_fit_layer: M = max(batch, M_val) */
+    PD_OP_FIT_LAYER = 5, /* pd_fit_layer: M = max(batch, M_val) */
+    PD_OP_ATTN = 6       /* pd_attn_prompt, pd_kv_append, pd_attn_cache: any sizes */
 } pd_op;
 
 /*
@@ -345,6 +347,104 @@ pd_status pd_fit_layer(const void *x_tr, const void *y_tr, int64_t M_tr, const v
                        const void *w_b, const uint32_t *mask, const void *v_row0, const void *v_col0, int64_t d_out,
                        int64_t d_in, int32_t epochs, int64_t batch, const pd_adamw *opt, int32_t cosine, void *v_out,
                        int32_t *axis_out, float *val_loss, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * ---- Attention between the linears of a block ----
+ * What a decoder block needs between its q/k/v linears and its o linear (pd_linear and its relatives): attention over
+ * prompts, a key/value cache in 8 bits, and attention of single tokens over that cache.  The paper serves whole models
+ * and says nothing about attention; these calls belong to this library.
+ *
+ * Sizes.  head_dim is 64 or 128; q_heads is a multiple of kv_heads, and query head h reads key/value head
+ * h / (q_heads / kv_heads).  Activations are [tokens, heads, head_dim] in binary16 (bfloat16 in the _bf16 calls) with
+ * contiguous heads; their token and head strides are in elements, positive multiples of 8 (a stride along a dimension
+ * of size 1 is not looked at), their pointers 16-byte aligned.  Scores, softmax statistics and sums are binary32.
+ * Several sequences are packed: cu_seqlens int32 [n_seqs + 1] (device), sequence b's tokens are rows
+ * cu_seqlens[b] .. cu_seqlens[b + 1]; sequences may be empty.
+ *
+ * Cache.  Pages of `page` (16, 32, 64 or 128) consecutive tokens of one sequence: codes int8
+ * [n_pages, kv_heads, page, head_dim] and scales fp32 [n_pages, kv_heads], for keys and for values.  A code c of a page
+ * and head with scale s stands for c * s.  block_table int32 [n_seqs, table_stride] (device): entry i of sequence b is
+ * the page of its tokens i * page .. (i + 1) * page; only the entries that its length reaches are read, of at most
+ * table_width.  seq_lens int32 [n_seqs] (device): tokens of each sequence, for pd_kv_append AFTER the call, so that the
+ * append and the attention behind it take the same lengths.
+ *
+ * Workspace: pd_workspace_bytes(PD_OP_ATTN, 0, 0, 0, 0) bytes that are all zero before the first call.  Every call leaves
+ * its status words and counters as the next one needs them; calls queued on one stream can share it, calls that overlap
+ * on the GPU and calls of other operations need workspaces of their own.
+ * Errors that only the device sees (offsets or lengths out of range, a page number outside [0, n_pages)) latch
+ * PD_ERR_BAD_INDEX; nothing outside the given tensors is read or written, and what that sequence gets is unspecified.
+ */
+
+/*
+ * pd_attn_prompt -- causal attention over whole prompts: token i of a sequence attends to tokens 0 .. i of it.
+ *
+ *   q    : in,  [n_tokens, q_heads, head_dim];  k, v : in, [n_tokens, kv_heads, head_dim]
+ *   out  : out, [n_tokens, q_heads, head_dim] = softmax(scale q . k^T, over the tokens up to the query's) . v
+ * Rows of n_tokens that no sequence claims are left as they are.  What k and v hold at tokens that a query does not
+ * attend to has no influence on it, infinities and NaN included.
+ */
+pd_status pd_attn_prompt(const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                         const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                         const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                         const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens,
+                         int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                         void *out, int64_t out_token_stride, int64_t out_head_stride,
+                         void *workspace, size_t workspace_bytes, void *cuda_stream);
+pd_status pd_attn_prompt_bf16(const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                              const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                              const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                              const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens,
+                              int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale,
+                              void *out, int64_t out_token_stride, int64_t out_head_stride,
+                              void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * pd_kv_append -- quantises new keys and values into the cache.
+ *
+ *   k, v       : in,  [n_tokens, kv_heads, head_dim], packed by cu_seqlens: sequence b gains
+ *                cu_seqlens[b + 1] - cu_seqlens[b] tokens (prompts, pieces of prompts, single tokens, none) and ends at
+ *                position seq_lens[b]
+ *   k_values, v_values : out, dense [n_tokens, kv_heads, head_dim], the values that the new codes stand for, rounded to
+ *                the activations' type; each may be NULL, k_values may be k and v_values v where those are dense
+ * A page and head with new tokens gets the scale s' = max(s, max |new| / 127) (s = 0 where the page's first token is among
+ * the new ones, whatever the page held before), its held codes become round(c * (s * (1/s'))) and the new ones
+ * round(x * (1/s')), all in binary32 with rounding to nearest even.  A page whose s' is below 2^-120 gets codes of zero; one
+ * with an infinity or a NaN among its values reads as NaN.  No page may belong to two sequences of a call.
+ */
+pd_status pd_kv_append(const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                       const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                       const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens, int32_t kv_heads, int32_t head_dim,
+                       int8_t *k_codes, int8_t *v_codes, float *k_scale, float *v_scale, int64_t n_pages, int32_t page,
+                       const int32_t *seq_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                       void *k_values, void *v_values, void *workspace, size_t workspace_bytes, void *cuda_stream);
+pd_status pd_kv_append_bf16(const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                            const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                            const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens, int32_t kv_heads, int32_t head_dim,
+                            int8_t *k_codes, int8_t *v_codes, float *k_scale, float *v_scale, int64_t n_pages, int32_t page,
+                            const int32_t *seq_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                            void *k_values, void *v_values, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * pd_attn_cache -- attention of one token per sequence over the cache.
+ *
+ *   q   : in,  [n_seqs, q_heads, head_dim]
+ *   out : out, [n_seqs, q_heads, head_dim] = softmax(scale q . K^T, over the seq_lens[b] cached tokens) . V; zeros where
+ *         seq_lens[b] is 0
+ * Slots of a page past the sequence's end and pages that it does not reach have no influence, whatever they hold.
+ * Parts of a long sequence are joined in a fixed order: the same call gives the same bits.
+ */
+pd_status pd_attn_cache(const void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n_seqs, int32_t q_heads,
+                        int32_t kv_heads, int32_t head_dim, float scale, const int8_t *k_codes, const int8_t *v_codes,
+                        const float *k_scale, const float *v_scale, int64_t n_pages, int32_t page, const int32_t *seq_lens,
+                        const int32_t *block_table, int64_t table_stride, int32_t table_width, void *out,
+                        int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes,
+                        void *cuda_stream);
+pd_status pd_attn_cache_bf16(const void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n_seqs, int32_t q_heads,
+                             int32_t kv_heads, int32_t head_dim, float scale, const int8_t *k_codes, const int8_t *v_codes,
+                             const float *k_scale, const float *v_scale, int64_t n_pages, int32_t page, const int32_t *seq_lens,
+                             const int32_t *block_table, int64_t table_stride, int32_t table_width, void *out,
+                             int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes,
+                             void *cuda_stream);
 
 /* Human-readable name of a status code; never NULL. */
 const char *pd_status_string(pd_status status);

@@ -14,7 +14,7 @@ import torch
 AXIS_ROW = 0
 AXIS_COL = 1
 AXIS_SCALAR = 2  # pd_fit_* only
-OP_PACK, OP_LINEAR, OP_LINEAR_MULTIVARIANT, OP_MERGE, OP_FIT, OP_FIT_LAYER = 0, 1, 2, 3, 4, 5
+OP_PACK, OP_LINEAR, OP_LINEAR_MULTIVARIANT, OP_MERGE, OP_FIT, OP_FIT_LAYER, OP_ATTN = 0, 1, 2, 3, 4, 5, 6
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpd.so")
@@ -23,7 +23,8 @@ EXPORTS = ["pd_pack_delta", "pd_pack_delta_static", "pd_linear_host", "pd_linear
            "pd_workspace_bytes", "pd_device_status", "pd_status_string", "pd_launch_count", "pd_selftest_bounded_wait",
            "pd_pack_delta_bf16", "pd_merge_bf16", "pd_linear_bf16", "pd_linear_multivariant_bf16",
            "pd_artifact_bytes", "pd_load_merged",
-           "pd_transpose_mask", "pd_fit_loss_grad", "pd_fit_adamw_step", "pd_fit_layer"]
+           "pd_transpose_mask", "pd_fit_loss_grad", "pd_fit_adamw_step", "pd_fit_layer",
+           "pd_attn_prompt", "pd_attn_prompt_bf16", "pd_kv_append", "pd_kv_append_bf16", "pd_attn_cache", "pd_attn_cache_bf16"]
 LINEAR_WEIGHTS_RESIDENT = 1
 
 
@@ -85,6 +86,13 @@ def _load() -> ctypes.CDLL:
     lib.pd_fit_adamw_step.restype = ctypes.c_int
     lib.pd_fit_layer.argtypes = [p, p, i64, p, p, i64, p, p, p, p, i64, i64, i32, i64, ctypes.POINTER(PdAdamW), i32, p, p, p, p, sz, p]
     lib.pd_fit_layer.restype = ctypes.c_int
+    f32, view = ctypes.c_float, [p, i64, i64]
+    for suffix in ("", "_bf16"):
+        for name, argtypes in (("pd_attn_prompt", 3 * view + [p, i32, i64, i32, i32, i32, f32] + view + [p, sz, p]),
+                               ("pd_kv_append", 2 * view + [p, i32, i64, i32, i32] + 4 * [p] + [i64, i32, p, p, i64, i32] + 2 * [p] + [p, sz, p]),
+                               ("pd_attn_cache", view + [i32, i32, i32, i32, f32] + 4 * [p] + [i64, i32, p, p, i64, i32] + view + [p, sz, p])):
+            fn = getattr(lib, name + suffix)
+            fn.argtypes, fn.restype = argtypes, ctypes.c_int
     lib.pd_launch_count.argtypes = []
     lib.pd_launch_count.restype = i64
     for name, proto in (("pd_pack_delta_bf16", lib.pd_pack_delta), ("pd_merge_bf16", lib.pd_merge),
@@ -351,6 +359,126 @@ def pd_fit_layer(x_tr, y_tr, x_val, y_val, w_b, mask, v_row0, v_col0, epochs, ba
                             _ptr(v_row0), _ptr(v_col0), d_out, d_in, int(epochs), int(batch), ctypes.byref(opt), int(bool(cosine)),
                             _ptr(v_out), _ptr(axis_out), _ptr(val_loss), _ptr(ws), ws.numel(), _stream()), "pd_fit_layer")
     return v_out, axis_out, val_loss
+
+
+_attn_ws_cache: dict = {}
+
+
+def _attn_workspace(device, stream: int) -> torch.Tensor:
+    """The attention calls' own scratch tensor, one for each device and stream: it must be all zero before its first
+    call, and calls that overlap on the GPU must not share it."""
+    key = (device.index, stream)
+    ws = _attn_ws_cache.get(key)
+    if ws is None:
+        ws = _attn_ws_cache[key] = torch.zeros(workspace_bytes(OP_ATTN), dtype=torch.uint8, device=device)
+    return ws
+
+
+def attn_workspace(device=None) -> torch.Tensor:
+    """The workspace that attention calls without one of their own use on the current stream (for pd_device_status)."""
+    device = device or torch.device("cuda", torch.cuda.current_device())
+    return _attn_workspace(device, torch.cuda.current_stream(device).cuda_stream)
+
+
+def _heads(t, name, dtype=None, device=None):
+    """Checks an activation [tokens, heads, head_dim]; a stride over heads or tokens may be anything that the library takes."""
+    if t.dim() != 3 or not t.is_cuda or t.dtype != (dtype or t.dtype) or t.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"{name} must be a CUDA tensor [tokens, heads, head_dim] of {dtype or 'float16 or bfloat16'}")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: the values of a head must be contiguous")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, other tensors on {device}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _index(t, name, shape, device):
+    if t.dtype != torch.int32 or t.device != device:
+        raise TypeError(f"{name} must be an int32 tensor on {device}")
+    if t.dim() != len(shape) or any(want is not None and got != want for got, want in zip(t.shape, shape)) or t.stride(-1) != 1:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit, or is not contiguous")
+    return t.data_ptr()
+
+
+def _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, device):
+    for t, name, dtype, ndim in ((k_codes, "k_codes", torch.int8, 4), (v_codes, "v_codes", torch.int8, 4), (k_scale, "k_scale", torch.float32, 2),
+                                 (v_scale, "v_scale", torch.float32, 2)):
+        if t.dtype != dtype or t.device != device:
+            raise TypeError(f"{name} must be a tensor of {dtype} on {device}")
+        if t.dim() != ndim or t.shape[:2] != k_codes.shape[:2] or not t.is_contiguous():
+            raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit, or is not contiguous")
+    if k_codes.shape != v_codes.shape or k_codes.shape[1] != kv_heads or k_codes.shape[3] != head_dim:
+        raise ValueError(f"the cache holds {tuple(k_codes.shape)} codes [pages, kv_heads, page, head_dim], the call has {kv_heads} heads of {head_dim}")
+    return k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_codes.shape[0], k_codes.shape[2]
+
+
+def _attn_call(name, bf16, device, args, workspace):
+    """Calls entry point `name` with `args`, a workspace and the current stream of `device`."""
+    with torch.cuda.device(device):
+        stream = torch.cuda.current_stream(device).cuda_stream
+        ws = workspace if workspace is not None else _attn_workspace(device, stream)
+        _check(getattr(lib, name + "_bf16" if bf16 else name)(*args, ws.data_ptr(), ws.numel() * ws.element_size(), stream), name)
+
+
+def pd_attn_prompt(q, k, v, cu_seqlens, scale=None, out=None, workspace=None):
+    """Causal attention over packed prompts: q [T, q_heads, head_dim], k and v [T, kv_heads, head_dim], cu_seqlens int32
+    [n_seqs + 1]; scale: 1 / sqrt(head_dim) unless given.  Returns out [T, q_heads, head_dim]."""
+    n_tokens, q_heads, head_dim = q.shape if q.dim() == 3 else (0, 0, 0)
+    dev = q.device
+    views = _heads(q, "q") + _heads(k, "k", q.dtype, dev) + _heads(v, "v", q.dtype, dev)
+    if k.shape != v.shape or k.shape[0] != n_tokens or k.shape[2] != head_dim:
+        raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+        raise ValueError("cu_seqlens: one offset more than there are sequences is wanted")
+    if out is None:
+        out = torch.empty((n_tokens, q_heads, head_dim), dtype=q.dtype, device=dev)
+    elif out.shape != q.shape:
+        raise ValueError(f"out: shape {tuple(out.shape)}, wanted {tuple(q.shape)}")
+    args = views + (_index(cu_seqlens, "cu_seqlens", (None,), dev), cu_seqlens.numel() - 1, n_tokens, q_heads, k.shape[1], head_dim,
+                    head_dim ** -0.5 if scale is None else scale) + _heads(out, "out", q.dtype, dev)
+    _attn_call("pd_attn_prompt", q.dtype == torch.bfloat16, dev, args, workspace)
+    return out
+
+
+def pd_kv_append(k, v, k_codes, v_codes, k_scale, v_scale, cu_seqlens, seq_lens, block_table, k_values=None, v_values=None, workspace=None):
+    """Quantises new keys and values k, v [T, kv_heads, head_dim] (packed by cu_seqlens) into the pages of the cache: codes
+    int8 [n_pages, kv_heads, page, head_dim], scales fp32 [n_pages, kv_heads].  seq_lens int32 [n_seqs]: lengths AFTER the
+    call; block_table int32 [n_seqs, width].  k_values, v_values [T, kv_heads, head_dim], dense, take the values that the new
+    codes stand for (may be k and v)."""
+    n_tokens, kv_heads, head_dim = k.shape if k.dim() == 3 else (0, 0, 0)
+    dev = k.device
+    views = _heads(k, "k") + _heads(v, "v", k.dtype, dev)
+    if k.shape != v.shape:
+        raise ValueError(f"shapes do not fit: k {tuple(k.shape)}, v {tuple(v.shape)}")
+    for t, name in ((k_values, "k_values"), (v_values, "v_values")):
+        if t is not None:
+            _heads(t, name, k.dtype, dev)
+            if t.shape != k.shape or not t.is_contiguous():
+                raise ValueError(f"{name}: a dense tensor {tuple(k.shape)} is wanted")
+    n_seqs = seq_lens.numel()
+    codes = _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, dev)
+    args = views + (_index(cu_seqlens, "cu_seqlens", (n_seqs + 1,), dev), n_seqs, n_tokens, kv_heads, head_dim) + codes + (
+        _index(seq_lens, "seq_lens", (None,), dev), _index(block_table, "block_table", (n_seqs, None), dev), block_table.stride(0) if n_seqs > 1 else
+        block_table.shape[1], block_table.shape[1], _ptr(k_values), _ptr(v_values))
+    _attn_call("pd_kv_append", k.dtype == torch.bfloat16, dev, args, workspace)
+
+
+def pd_attn_cache(q, k_codes, v_codes, k_scale, v_scale, seq_lens, block_table, scale=None, out=None, workspace=None):
+    """Attention of one token per sequence, q [n_seqs, q_heads, head_dim], over the first seq_lens[b] tokens of its pages
+    (the cache of pd_kv_append).  Returns out [n_seqs, q_heads, head_dim]; zeros for an empty sequence."""
+    n_seqs, q_heads, head_dim = q.shape if q.dim() == 3 else (0, 0, 0)
+    dev = q.device
+    view = _heads(q, "q")
+    kv_heads = k_codes.shape[1] if k_codes.dim() == 4 else 0
+    if out is None:
+        out = torch.empty((n_seqs, q_heads, head_dim), dtype=q.dtype, device=dev)
+    elif out.shape != q.shape:
+        raise ValueError(f"out: shape {tuple(out.shape)}, wanted {tuple(q.shape)}")
+    codes = _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, dev)
+    args = view + (n_seqs, q_heads, kv_heads, head_dim, head_dim ** -0.5 if scale is None else scale) + codes + (
+        _index(seq_lens, "seq_lens", (n_seqs,), dev), _index(block_table, "block_table", (n_seqs, None), dev),
+        block_table.stride(0) if n_seqs > 1 else block_table.shape[1], block_table.shape[1]) + _heads(out, "out", q.dtype, dev)
+    _attn_call("pd_attn_cache", q.dtype == torch.bfloat16, dev, args, workspace)
+    return out
 
 
 def pd_selftest_bounded_wait(limit_cycles=100000, workspace=None, device=None):

@@ -2,6 +2,7 @@
 // allocated here; everything runs on the caller's stream.
 #include <climits>
 
+#include "pd_attn.cuh"
 #include "pd_ptx.cuh"
 
 namespace pd {
@@ -170,6 +171,8 @@ size_t pd_workspace_bytes(int op, int64_t M, int32_t V, int64_t d_out, int64_t d
                    (M > kGemvMaxTokens ? grouped_table_bytes(M, V) + round_up(static_cast<size_t>(M) * d_in * 2, 256) : 0);
         case PD_OP_FIT:
             return M > 0 ? kStatusBytes + fit_scratch_bytes(M, d_out, d_in) : 0;
+        case PD_OP_ATTN:
+            return kStatusBytes + attn_cache_scratch_bytes();
         case PD_OP_FIT_LAYER:
             return M > 0 ? kStatusBytes + fit_layer_scratch_bytes(M, M, d_out, d_in) : 0;
         case PD_OP_MERGE:
@@ -188,6 +191,7 @@ const char *pd_status_string(pd_status s) {
         case PD_ERR_CUDA: return "CUDA call failed";
         case PD_ERR_BAD_VARIANT: return "variant id out of range";
         case PD_ERR_DEVICE_TIMEOUT: return "device-side wait timed out";
+        case PD_ERR_BAD_INDEX: return "sequence offset, length or page number out of range";
     }
     return "unknown status";
 }
