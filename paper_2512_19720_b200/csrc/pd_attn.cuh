@@ -17,6 +17,7 @@ struct PromptArgs {
     int n_seqs, n_tokens, q_heads, kv_heads, head_dim;
     float scale;
     uint32_t *status;
+    unsigned int *counters;  // two, zero on entry, zero again on return
 };
 
 // The 8-bit paged cache: codes [n_pages, kv_heads, page, head_dim], scales [n_pages, kv_heads].

@@ -63,7 +63,7 @@ pd_status prompt_impl(HeadsView q, HeadsView k, HeadsView v, const int32_t *cu_s
     if (reinterpret_cast<uintptr_t>(cu_seqlens) & 3u) return PD_ERR_ALIGNMENT;
     PD_TRY(check_workspace(workspace, workspace_bytes));
     const PromptArgs a = {q, k, v, out, cu_seqlens, n_seqs, static_cast<int>(n_tokens), q_heads, kv_heads, head_dim, scale,
-                          static_cast<uint32_t *>(workspace)};
+                          static_cast<uint32_t *>(workspace), reinterpret_cast<unsigned int *>(static_cast<unsigned char *>(workspace) + kStatusBytes)};
     return launch_attn_prompt(a, bf16, static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -1,29 +1,95 @@
 // Causal attention over packed prompts: out[i, h] = sum_{j <= i} softmax_j(scale q[i, h] . k[j, g]) v[j, g] inside each sequence.
 //
-// One pass over the keys with a running maximum m and sum l of each query row (32 bits): with s the scores of a tile,
-//     m' = max(m, max s),  l' = l e^(m - m') + sum e^(s - m'),  O' = O e^(m - m') + e^(s - m') V,  out = O / l at the end.
-// P = e^(s - m') is rounded to the type of v for its product; l sums the unrounded values.
+// One pass over the keys with a running maximum m and sum l of each query row (32 bits, base 2): with s the scores of a tile,
+//     m' = max(m, max s),  l' = l 2^(m - m') + sum 2^(s - m'),  O' = O 2^(m - m') + 2^(s - m') V,  out = O / l at the end.
+// P = 2^(s - m') is rounded to the type of v for its product; l sums the unrounded values.  m only moves when a score passes
+// it by more than 8, so that O is hardly ever rescaled: P is then at most 2^8 and its relative rounding is the same.
 //
-// A thread block takes 64 queries of one head, a warp 16 of them, against tiles of 64 keys.
+// Bound by the tensor cores (4 * head_dim operations per query, key and head) and, as nearly, by the exponentials: a tile of
+// 128 x 128 scores is 1024 clocks of products at head_dim 128 and 1024 clocks of the 16 exponentials a clock that an SM has.
+//
+// A block works on units of two *slots* of 128 queries each that read the same keys: two heads that share their key/value
+// head where their number is even, else two consecutive pieces of one head's queries.  While one slot's scores are in the
+// softmax the tensor cores work for the other.  Tiles of 128 keys: S = Q K^T (both operands in shared memory) into tensor
+// memory, softmax by one thread per row, P back into tensor memory in S's place, O += P V with P from tensor memory.  P is
+// handed over in two halves, so that the second product starts while the second half's exponentials are computed.
+// Tensor memory is full: 2 x 128 columns of S (P inside), 2 x 128 of O.
+//
+// Roles: warps 0-3 and 4-7 the softmax and the output of slot 0 and 1; warp 8 units and TMA; warp 9 issues the products;
+// warps 10 and 11 look for infinities and NaN among the values of the tile on the diagonal, where 0 * v must not reach the
+// queries that do not attend to v: they are set to zero there, and the output adds them for the queries that do.
+// The products of a block are issued by one thread and run in the order of issue: S of the next tile follows the product
+// that reads P from the same place.  Every wait is bounded.
 #include "pd_attn.cuh"
-#include "pd_ptx.cuh"
+#include "pd_tcgen05.cuh"
 
 namespace pd {
 namespace {
 
-constexpr int kQ = 64, kK = 64;  // queries of a block, keys of a tile
+constexpr int kTile = 128;  // queries of a slot, keys of a tile
+constexpr int kWarps = 12;
+constexpr int kThreads = kWarps * 32;
+constexpr int kUnits = 4;  // units that the producer may be ahead
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kMaxLead = 8.f;  // how far (base-2 exponent) a score may pass the reference maximum
+constexpr uint32_t kColS = 0, kColO = 256;  // tensor-memory columns; slot 1: + 128
+
+struct Unit {
+    int first, len;  // the sequence's first token and its length; len 0: no more units
+    int q0, head;    // first query (in the sequence) and head of slot 0
+};
+
+struct Slots {
+    bool by_head;  // slots are two heads (else two consecutive tiles of queries)
+    __device__ __forceinline__ int q0(const Unit &u, int s) const { return by_head ? u.q0 : u.q0 + s * kTile; }
+    __device__ __forceinline__ int head(const Unit &u, int s) const { return by_head ? u.head + s : u.head; }
+    // key tiles of a slot; 0: the slot has no queries
+    __device__ __forceinline__ int tiles(const Unit &u, int s) const { return q0(u, s) < u.len ? q0(u, s) / kTile + 1 : 0; }
+    __device__ __forceinline__ int max_tiles(const Unit &u) const { return max(tiles(u, 0), tiles(u, 1)); }
+};
+
+template <int D>
+struct PromptSmem {
+    static constexpr int kTileBytes = kTile * D * 2;
+    static constexpr int kStages = D == 128 ? 5 : 8;  // of keys or values
+    static constexpr int kQ = 0;
+    static constexpr int kRing = 2 * kTileBytes;
+    static constexpr int kBars = kRing + kStages * kTileBytes;
+    static constexpr int kTotal = kBars + 1024 + 1024;  // + slack for 1024-byte alignment
+    static_assert(kTotal <= 227 * 1024, "shared memory");
+};
+
+struct Bars {
+    uint64_t kv_full[8], kv_empty[8];
+    uint64_t q_full[2], q_empty[2];
+    uint64_t s_full[2], p_half[2][2], o_done[2], o_empty[2];
+    uint64_t v_ask, v_clean;  // a tile on a diagonal has landed, has been looked through
+    uint64_t unit_full[kUnits], unit_empty[kUnits];
+    Unit units[kUnits];
+    int taint[kUnits][2];
+    uint32_t tmem;
+    int abort_flag;
+};
+static_assert(sizeof(Bars) <= 1024, "barriers");
 
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], const void *p) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_u32(p)) : "memory");
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 x, x, y, z;\nmov.b64 {%0, %1}, x;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
 }
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], const void *p) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_u32(p)) : "memory");
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n.reg .b64 x, y;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
 }
 // one of the two 16-bit values is an infinity or a NaN
 template <bool BF16>
@@ -32,152 +98,434 @@ __device__ __forceinline__ bool non_finite2(uint32_t w) {
     return (w & e) == e || ((w >> 16) & e) == e;
 }
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(128) attn_prompt_kernel(const PromptArgs a) {
-    using E = Elem<BF16>;
-    constexpr int P = D + 8;  // row pitch in shared memory
-    extern __shared__ __align__(16) uint16_t sm[];
-    uint16_t *sq = sm, *sk = sm + kQ * P, *sv = sk + kK * P;
-    __shared__ int found, tainted;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    // sequence b's blocks are the ids from cu[b] / 64 + b on: never more than the ids before the next sequence's
-    if (threadIdx.x == 0) found = 0, tainted = 0;
-    __syncthreads();
-    int mine = 0;
-    for (int b = threadIdx.x; b < a.n_seqs; b += blockDim.x)
-        if (min(max(__ldg(a.cu_seqlens + b), 0), a.n_tokens) / kQ + b <= static_cast<int>(blockIdx.x)) mine = b;
-    if (mine) atomicMax(&found, mine);
-    __syncthreads();
-    const int b = found;
-    const int first = __ldg(a.cu_seqlens + b), last = __ldg(a.cu_seqlens + b + 1);
-    if (first < 0 || last < first || last > a.n_tokens) {
-        if (threadIdx.x == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
-        return;
-    }
-    const int len = last - first, q0 = (static_cast<int>(blockIdx.x) - first / kQ - b) * kQ;
-    if (q0 >= len) return;
-    const int head = blockIdx.y, kvh = head / (a.q_heads / a.kv_heads);
-    const uint16_t *qp = static_cast<const uint16_t *>(a.q.ptr) + first * a.q.token_stride + head * a.q.head_stride;
-    const uint16_t *kp = static_cast<const uint16_t *>(a.k.ptr) + first * a.k.token_stride + kvh * a.k.head_stride;
-    const uint16_t *vp = static_cast<const uint16_t *>(a.v.ptr) + first * a.v.token_stride + kvh * a.v.head_stride;
-    auto load = [&](uint16_t *dst, const uint16_t *src, int64_t stride, int row0) {
-        for (int i = threadIdx.x; i < 64 * (D / 8); i += blockDim.x) {
-            const int r = i / (D / 8), c = i % (D / 8);
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (row0 + r < len) x = __ldg(reinterpret_cast<const uint4 *>(src + (row0 + r) * stride) + c);
-            *reinterpret_cast<uint4 *>(dst + r * P + 8 * c) = x;
-        }
-    };
-    load(sq, qp, a.q.token_stride, q0);
-    __syncthreads();
-    uint32_t qf[D / 16][4];
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) ldmatrix_x4(qf[k], sq + (warp * 16 + (lane & 15)) * P + 16 * k + 8 * (lane >> 4));
-    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    const float f = a.scale * kLog2e;
-    const int row0 = q0 + warp * 16 + g;  // and row0 + 8
+// A and B in shared memory
+__device__ __forceinline__ void mma_smem_a(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// B operand with the head dimension contiguous (the contraction runs over rows of 128 bytes): groups of 8 rows 1024 bytes
+// apart, pieces of 64 columns a whole sub-tile apart; 128-byte swizzle
+__device__ __forceinline__ uint64_t make_v_desc(uint32_t addr, uint32_t piece_bytes) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((addr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>(piece_bytes >> 4) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
 
-    for (int k0 = 0; k0 <= q0; k0 += kK) {
-        __syncthreads();
-        load(sk, kp, a.k.token_stride, k0);
-        load(sv, vp, a.v.token_stride, k0);
-        __syncthreads();
-        if (k0 == q0) {  // some queries do not attend to some of these keys: 0 * infinity must not reach them
-            for (int i = threadIdx.x; i < kK * (D / 2); i += blockDim.x) {
-                uint32_t *w = reinterpret_cast<uint32_t *>(sv + i / (D / 2) * P) + i % (D / 2);
-                if (non_finite2<BF16>(*w)) {
-                    tainted = 1;
-                    if (non_finite2<BF16>(*w & 0xffffu)) *w &= 0xffff0000u;
-                    if (non_finite2<BF16>(*w & 0xffff0000u)) *w &= 0xffffu;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const PromptArgs a, const int n_ids) {
+    using E = Elem<BF16>;
+    using L = PromptSmem<D>;
+    constexpr int kStages = L::kStages;
+    constexpr int kPieces = D / 64;                    // sub-tiles of 64 columns
+    constexpr int kPieceBytes = kTile * 64 * 2;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    Bars &bar = *reinterpret_cast<Bars *>(smem + L::kBars);
+    volatile int *abort_flag = &bar.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = a.q_heads / a.kv_heads;
+    const Slots slots = {group % 2 == 0};
+    auto wait = [&](uint64_t *b, uint32_t parity, uint32_t where) { return mbar_wait(b, parity & 1u, abort_flag, a.status, where); };
+    auto wait_warp = [&](uint64_t *b, uint32_t parity, uint32_t where) { return __all_sync(0xffffffffu, wait(b, parity, where)) != 0; };
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) mbar_init(bar.kv_full + i, 1), mbar_init(bar.kv_empty + i, 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar.q_full + s, 1), mbar_init(bar.q_empty + s, 1), mbar_init(bar.s_full + s, 1);
+            mbar_init(bar.p_half[s], 4), mbar_init(bar.p_half[s] + 1, 4), mbar_init(bar.o_done + s, 1), mbar_init(bar.o_empty + s, 4);
+        }
+        mbar_init(&bar.v_ask, 1), mbar_init(&bar.v_clean, 2);
+        for (int i = 0; i < kUnits; ++i) mbar_init(bar.unit_full + i, 1), mbar_init(bar.unit_empty + i, 11);
+        bar.abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 9) tcgen05_alloc(&bar.tmem, 512);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = bar.tmem;
+
+    // The next unit, in the producer's order: every other role reads what the producer wrote.
+    uint32_t n_unit = 0;
+    auto next_unit = [&](Unit &u) {
+        if (!wait_warp(bar.unit_full + n_unit % kUnits, n_unit / kUnits, 50)) return false;
+        u = bar.units[n_unit % kUnits];
+        return u.len > 0;
+    };
+    auto done_unit = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar.unit_empty + n_unit % kUnits);
+        ++n_unit;
+    };
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 8) {
+            // -------------------------------------------------------- units and TMA
+            // Sequence b's units are the ids from (cu[b] / span + b) * per_tile on, `span` queries to a unit: never more of them
+            // than ids before the next sequence's.  Ids that no unit has are passed over.
+            const int span = slots.by_head ? kTile : 2 * kTile;
+            const int per_tile = slots.by_head ? a.q_heads / 2 : a.q_heads;
+            uint32_t it = 0, n_q[2] = {0, 0};
+            bool ok = true;
+            int id = lane == 0 ? static_cast<int>(atomicAdd(a.counters, 1u)) : 0;
+            while (ok) {
+                id = __shfl_sync(0xffffffffu, id, 0);
+                Unit u = {0, 0, 0, 0};
+                if (id < n_ids) {
+                    const int tile_id = id / per_tile;
+                    // the last sequence whose ids start at or before this one: 32 candidates a step
+                    int lo = 0, n = a.n_seqs;  // the answer is in [lo, lo + n)
+                    while (n > 1) {
+                        const int step = (n + 31) / 32;
+                        const int b = lo + lane * step;
+                        const bool le = lane * step < n && min(max(__ldg(a.cu_seqlens + b), 0), a.n_tokens) / span + b <= tile_id;
+                        const unsigned m = __ballot_sync(0xffffffffu, le);
+                        const int last = m ? 31 - __clz(m) : 0;
+                        lo += last * step;
+                        n = min(step, n - last * step);
+                    }
+                    const int first = __ldg(a.cu_seqlens + lo), end = __ldg(a.cu_seqlens + lo + 1);
+                    if (first < 0 || end < first || end > a.n_tokens) {
+                        if (lane == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(lo));
+                    } else {
+                        const int n_tiles = (end - first + span - 1) / span, k = tile_id - (first / span + lo);
+                        if (k >= 0 && k < n_tiles)  // the last queries first: theirs is the most work
+                            u = {first, end - first, (n_tiles - 1 - k) * span, (id % per_tile) * (slots.by_head ? 2 : 1)};
+                    }
+                    if (u.len == 0) {
+                        if (lane == 0) id = static_cast<int>(atomicAdd(a.counters, 1u));
+                        continue;
+                    }
+                }
+                const bool end_mark = u.len == 0;
+                if (lane == 0 && !end_mark) id = static_cast<int>(atomicAdd(a.counters, 1u));  // known by the time it is needed
+                const uint32_t us = n_unit % kUnits, ur = n_unit / kUnits;
+                if (ur > 0 && !(ok = wait_warp(bar.unit_empty + us, ur - 1, 51))) break;
+                if (lane == 0) {
+                    bar.units[us] = u;
+                    mbar_arrive(bar.unit_full + us);
+                }
+                ++n_unit;
+                if (end_mark) break;
+                if (lane == 0) {
+                    const int n = slots.max_tiles(u), kvh = u.head / group;
+                    auto load = [&](const CUtensorMap *map, unsigned char *dst, uint64_t *full, int head, int row) {
+                        mbar_arrive_expect_tx(full, L::kTileBytes);
+#pragma unroll
+                        for (int p = 0; p < kPieces; ++p) tma_load_3d(map, full, dst + p * kPieceBytes, p * 64, head, row);
+                    };
+                    for (int j = 0; j < n && ok; ++j) {
+                        if (j == 0) {
+                            for (int s = 0; s < 2 && ok; ++s) {
+                                if (slots.tiles(u, s) == 0) continue;
+                                if (n_q[s] > 0 && !(ok = wait(bar.q_empty + s, n_q[s] - 1, 52))) break;
+                                ++n_q[s];
+                                load(&map_q, smem + L::kQ + s * L::kTileBytes, bar.q_full + s, slots.head(u, s), u.first + slots.q0(u, s));
+                            }
+                        }
+                        for (int kv = 0; kv < 2 && ok; ++kv, ++it) {
+                            const uint32_t st = it % kStages, round = it / kStages;
+                            if (round > 0 && !(ok = wait(bar.kv_empty + st, round - 1, 53))) break;
+                            load(kv == 0 ? &map_k : &map_v, smem + L::kRing + st * L::kTileBytes, bar.kv_full + st, kvh, u.first + j * kTile);
+                        }
+                    }
+                }
+                ok = __all_sync(0xffffffffu, ok);
+            }
+        } else if (warp == 9) {
+            // -------------------------------------------------------- the products, issued by one thread
+            constexpr uint32_t kIdescS = kIdescBase<BF16> | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+            constexpr uint32_t kIdescO = kIdescBase<BF16> | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+            uint32_t it = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0}, n_clean = 0;
+            bool ok = true;
+            Unit u;
+            while (ok && next_unit(u)) {
+                const int n0 = slots.tiles(u, 0), n1 = slots.tiles(u, 1), n = max(n0, n1);
+                if (lane == 0) {
+                    auto scores = [&](int s, int j) {  // S = Q K_j^T
+                        const uint32_t q = smem_u32(smem + L::kQ + s * L::kTileBytes);
+                        const uint32_t k = smem_u32(smem + L::kRing + ((it + 2 * j) % kStages) * L::kTileBytes);
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint32_t off = (kk / 4) * kPieceBytes + (kk % 4) * 32;
+                            mma_smem_a(tmem + kColS + s * 128, make_smem_desc(q + off), make_smem_desc(k + off), kIdescS, kk > 0);
+                        }
+                        tcgen05_commit(bar.s_full + s);
+                    };
+                    auto full = [&](int i) { return wait(bar.kv_full + (it + i) % kStages, (it + i) / kStages, 54); };
+                    ok = full(0);
+                    for (int s = 0; s < 2 && ok; ++s) {
+                        if ((s ? n1 : n0) == 0) continue;
+                        if (!(ok = wait(bar.q_full + s, n_q[s], 55))) break;
+                        ++n_q[s];
+                        tcgen05_fence_after();
+                        scores(s, 0);
+                        if ((s ? n1 : n0) == 1) tcgen05_commit(bar.q_empty + s);
+                    }
+                    if (ok) tcgen05_commit(bar.kv_empty + it % kStages);
+                    for (int j = 0; j < n && ok; ++j) {
+                        if (!(ok = full(2 * j + 1))) break;
+                        const bool diagonal = j == n0 - 1 || j == n1 - 1;
+                        if (diagonal) {
+                            mbar_arrive(&bar.v_ask);
+                            if (!(ok = wait(&bar.v_clean, n_clean++, 56))) break;
+                        }
+                        if (j + 1 < n && !(ok = full(2 * j + 2))) break;
+                        const uint32_t v = smem_u32(smem + L::kRing + ((it + 2 * j + 1) % kStages) * L::kTileBytes);
+                        for (int s = 0; s < 2 && ok; ++s) {
+                            const int ns = s ? n1 : n0;
+                            if (j >= ns) continue;
+                            if (j == 0 && n_q[s] > 1 && !(ok = wait(bar.o_empty + s, n_q[s] - 2, 57))) break;
+#pragma unroll
+                            for (int half = 0; half < 2 && ok; ++half) {
+                                if (!(ok = wait(bar.p_half[s] + half, n_p[s], 58))) break;
+                                tcgen05_fence_after();
+#pragma unroll
+                                for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
+                                    tcgen05_mma_f16_tmem_a(tmem + kColO + s * 128, tmem + kColS + s * 128 + kk * 8, make_v_desc(v + kk * 2048, kPieceBytes),
+                                                           kIdescO, (j > 0 || kk > 0) ? 1u : 0u);
+                            }
+                            if (!ok) break;
+                            ++n_p[s];
+                            tcgen05_commit(bar.o_done + s);
+                            if (j + 1 < ns) {
+                                scores(s, j + 1);
+                                if (j + 2 == ns) tcgen05_commit(bar.q_empty + s);
+                            }
+                        }
+                        if (!ok) break;
+                        tcgen05_commit(bar.kv_empty + (it + 2 * j + 1) % kStages);
+                        if (j + 1 < n) tcgen05_commit(bar.kv_empty + (it + 2 * j + 2) % kStages);
+                    }
+                }
+                ok = __all_sync(0xffffffffu, ok);
+                it += 2 * n;
+                done_unit();
+            }
+        } else {
+            // -------------------------------------------------------- values on the diagonal: no infinities and NaN in shared memory
+            uint32_t it = 0, n_ask = 0;
+            bool ok = true;
+            Unit u;
+            while (ok && next_unit(u)) {
+                const int n0 = slots.tiles(u, 0), n1 = slots.tiles(u, 1), n = max(n0, n1);
+                bool found = false;
+                for (int j = n0 - 1; j < n && ok; ++j) {
+                    const uint32_t i = it + 2 * j + 1;
+                    if (!(ok = wait_warp(&bar.v_ask, n_ask++, 59))) break;
+                    uint4 *p = reinterpret_cast<uint4 *>(smem + L::kRing + (i % kStages) * L::kTileBytes) + (warp - 10) * 32 + lane;
+#pragma unroll 8
+                    for (int k = 0; k < L::kTileBytes / 16 / 64; ++k) {
+                        uint4 x = p[k * 64];
+                        if (non_finite2<BF16>(x.x) || non_finite2<BF16>(x.y) || non_finite2<BF16>(x.z) || non_finite2<BF16>(x.w)) {
+                            found = true;
+                            uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                if (non_finite2<BF16>(w[c] & 0xffffu)) w[c] &= 0xffff0000u;
+                                if (non_finite2<BF16>(w[c] & 0xffff0000u)) w[c] &= 0xffffu;
+                            }
+                            p[k * 64] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                    found = __any_sync(0xffffffffu, found);
+                    if (lane == 0) bar.taint[n_unit % kUnits][warp - 10] = found;
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bar.v_clean);
+                }
+                it += 2 * n;
+                done_unit();
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        // ------------------------------------------------------------ softmax and output: a thread owns one row of a slot
+        const int s = warp >> 2;
+        const int r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        const uint32_t ts = lanes + kColS + s * 128, to = lanes + kColO + s * 128;
+        const float scale2 = a.scale * kLog2e;
+        const float f = scale2 > 0.f ? scale2 : (scale2 < 0.f ? -scale2 : 1.f);
+        uint32_t n_s = 0;
+        bool ok = true;
+        Unit u;
+        while (ok && next_unit(u)) {
+            const int n = slots.tiles(u, s), row = slots.q0(u, s) + r;
+            if (n == 0) {
+                done_unit();
+                continue;
+            }
+            float m = -INFINITY, mu = 0.f, l0 = 0.f;
+            float2 l = make_float2(0.f, 0.f);
+            for (int j = 0; j < n; ++j, ++n_s) {
+                if (!(ok = wait_warp(bar.s_full + s, n_s, 60))) break;
+                tcgen05_fence_after();
+                uint32_t x[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tcgen05_ld_32x32b_x32(ts + 32 * c, x[c]);
+                tcgen05_wait_ld();
+                if (scale2 <= 0.f) {  // the maximum is taken before the scores are scaled by |scale|
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[c][k] = scale2 < 0.f ? x[c][k] ^ 0x80000000u : __float_as_uint(__uint_as_float(x[c][k]) * 0.f);
+                }
+                if (j == n - 1) {  // on the diagonal: keys 0 .. r of the tile
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (32 * c + k > r) x[c][k] = __float_as_uint(-INFINITY);
+                }
+                float top[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    top[c] = __uint_as_float(x[c][0]);
+#pragma unroll
+                    for (int k = 1; k < 31; k += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])));
+                    top[c] = fmaxf(top[c], __uint_as_float(x[c][31]));
+                }
+                const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * f;
+                if (__any_sync(0xffffffffu, best > m + kMaxLead)) {
+                    const float now = fmaxf(m, best), mu_new = now == -INFINITY ? 0.f : now;
+                    const float shrink = exp2_approx(m - mu_new);  // 0 from -infinity on
+                    m = now, mu = mu_new;
+                    l.x *= shrink, l.y *= shrink;
+                    if (j > 0) {  // O of the tiles so far is complete, and the next product waits for this warp
+                        if (!(ok = wait_warp(bar.o_done + s, n_s - 1, 61))) break;
+                        tcgen05_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32];
+                            tcgen05_ld_32x32b_x32(to + c, o);
+                            tcgen05_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * shrink);
+                            tcgen05_st_32x32b_x32(to + c, o);
+                        }
+                        tcgen05_wait_st();
+                    }
+                }
+                const float2 ff = make_float2(f, f), sub = make_float2(-mu, -mu);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const uint32_t *w = &x[2 * half + k / 16][2 * (k % 16)];
+                        const float2 t = fma2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), ff, sub);
+                        const float2 e = make_float2(exp2_approx(t.x), exp2_approx(t.y));
+                        l = add2(l, e);
+                        p[k] = E::from_float2(e.x, e.y);
+                    }
+                    tcgen05_st_32x32b_x32(ts + 32 * half, p);
+                    tcgen05_wait_st();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar.p_half[s] + half);
                 }
             }
-            __syncthreads();
-        }
-        float s[kK / 8][4];
+            if (!ok) break;
+            // -------------------------------------------------------- output
+            if (!(ok = wait_warp(bar.o_done + s, n_s - 1, 62))) break;
+            tcgen05_fence_after();
+            l0 = l.x + l.y;
+            const float inv = 1.f / l0;
+            const bool taint = bar.taint[n_unit % kUnits][0] | bar.taint[n_unit % kUnits][1];
+            const int head = slots.head(u, s);
+            uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row) * a.out.token_stride + head * a.out.head_stride;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tcgen05_ld_32x32b_x32(to + c, o);
+                tcgen05_wait_ld();
+                if (row < u.len) {
 #pragma unroll
-        for (int j = 0; j < kK / 8; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * inv);
+                    if (taint) {
+                        const uint16_t *v = static_cast<const uint16_t *>(a.v.ptr) + (head / group) * a.v.head_stride + c;
+                        for (int key = u.q0; key <= row; ++key)
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-            for (int j = 0; j < kK / 16; ++j) {
-                uint32_t kf[4];
-                ldmatrix_x4(kf, sk + (j * 16 + (lane & 7) + 8 * (lane >> 4)) * P + 16 * k + 8 * ((lane >> 3) & 1));
-                E::mma16816(s[2 * j], qf[k][0], qf[k][1], qf[k][2], qf[k][3], kf[0], kf[1]);
-                E::mma16816(s[2 * j + 1], qf[k][0], qf[k][1], qf[k][2], qf[k][3], kf[2], kf[3]);
-            }
-        float top[2] = {m[0], m[1]};
-#pragma unroll
-        for (int j = 0; j < kK / 8; ++j)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int key = k0 + 8 * j + 2 * t + (k & 1);
-                s[j][k] = key <= row0 + 8 * (k >> 1) ? s[j][k] * f : -INFINITY;
-                top[k >> 1] = fmaxf(top[k >> 1], s[j][k]);
-            }
-        float mu[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-            mu[r] = top[r] == -INFINITY ? 0.f : top[r];
-            const float shrink = exp2_approx(m[r] - mu[r]);
-            m[r] = top[r], l[r] *= shrink;
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) o[i][2 * r] *= shrink, o[i][2 * r + 1] *= shrink;
-        }
-#pragma unroll
-        for (int j = 0; j < kK / 8; ++j)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                s[j][k] = exp2_approx(s[j][k] - mu[k >> 1]);
-                l[k >> 1] += s[j][k];
-            }
-#pragma unroll
-        for (int j = 0; j < kK / 16; ++j) {
-            const uint32_t p0 = E::from_float2(s[2 * j][0], s[2 * j][1]), p1 = E::from_float2(s[2 * j][2], s[2 * j][3]);
-            const uint32_t p2 = E::from_float2(s[2 * j + 1][0], s[2 * j + 1][1]), p3 = E::from_float2(s[2 * j + 1][2], s[2 * j + 1][3]);
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-                uint32_t vf[4];
-                ldmatrix_x4_trans(vf, sv + (j * 16 + (lane & 15)) * P + 16 * i + 8 * (lane >> 4));
-                E::mma16816(o[2 * i], p0, p1, p2, p3, vf[0], vf[1]);
-                E::mma16816(o[2 * i + 1], p0, p1, p2, p3, vf[2], vf[3]);
-            }
-        }
-    }
-    const bool taint = tainted != 0;
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        const int row = row0 + 8 * r;
-        if (row >= len) continue;
-        const float inv = 1.f / l[r];
-        uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + (first + row) * a.out.token_stride + head * a.out.head_stride;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            float x[2] = {o[i][2 * r] * inv, o[i][2 * r + 1] * inv};
-            if (taint) {  // infinities and NaN among the values of the last tile, for the queries that attend to them
-                for (int j = q0; j <= row; ++j)
-                    for (int k = 0; k < 2; ++k) {
-                        const float v = E::to_float(vp[j * a.v.token_stride + 8 * i + 2 * t + k]);
-                        if (!(fabsf(v) <= 3.402823466e38f)) x[k] += v;
+                            for (int k = 0; k < 32; ++k) {
+                                const float t = E::to_float(v[static_cast<int64_t>(u.first + key) * a.v.token_stride + k]);
+                                if (!(fabsf(t) <= 3.402823466e38f)) o[k] = __float_as_uint(__uint_as_float(o[k]) + t);
+                            }
                     }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = E::from_float2(__uint_as_float(o[8 * k + 2 * i]), __uint_as_float(o[8 * k + 2 * i + 1]));
+                        *reinterpret_cast<uint4 *>(y + c + 8 * k) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
             }
-            *reinterpret_cast<uint32_t *>(y + 8 * i + 2 * t) = E::from_float2(x[0], x[1]);
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.o_empty + s);
+            done_unit();
         }
     }
+
+    // ---------------------------------------------------------------- teardown
+    tcgen05_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);  // copies that may still be in flight
+        __syncthreads();
+    }
+    if (warp == 9) {
+        tcgen05_fence_after();
+        tcgen05_dealloc(tmem, 512);
+    }
+    if (threadIdx.x == 0) {  // the last block puts the counters back to zero for the next call
+        __threadfence();
+        if (atomicAdd(a.counters + 1, 1u) == gridDim.x - 1) {
+            a.counters[0] = 0u;
+            a.counters[1] = 0u;
+        }
+    }
+}
+
+bool make_heads_map(CUtensorMap *map, const HeadsView &x, int tokens, int heads, int head_dim, bool bf16) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(x.head_stride) * 2, static_cast<cuuint64_t>(x.token_stride) * 2};
+    const cuuint32_t box[3] = {64, 1, kTile};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(x.ptr), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D, bool BF16>
 pd_status launch(const PromptArgs &a, cudaStream_t stream) {
     static std::atomic<bool> done[kMaxDevices];
-    constexpr int bytes = 3 * 64 * (D + 8) * 2;
-    if (!ensure_dynamic_smem(attn_prompt_kernel<D, BF16>, bytes, done)) return PD_ERR_CUDA;
-    const dim3 grid(static_cast<unsigned>(a.n_tokens / kQ + a.n_seqs), static_cast<unsigned>(a.q_heads));
-    attn_prompt_kernel<D, BF16><<<grid, 128, bytes, stream>>>(a);
+    if (!ensure_dynamic_smem(attn_prompt_kernel<D, BF16>, PromptSmem<D>::kTotal, done)) return PD_ERR_CUDA;
+    CUtensorMap mq, mk, mv;
+    if (!make_heads_map(&mq, a.q, a.n_tokens, a.q_heads, D, BF16) || !make_heads_map(&mk, a.k, a.n_tokens, a.kv_heads, D, BF16) ||
+        !make_heads_map(&mv, a.v, a.n_tokens, a.kv_heads, D, BF16))
+        return PD_ERR_CUDA;
+    const bool by_head = (a.q_heads / a.kv_heads) % 2 == 0;
+    const int64_t tiles = a.n_tokens / (by_head ? kTile : 2 * kTile) + a.n_seqs;
+    const int64_t ids = tiles * (by_head ? a.q_heads / 2 : a.q_heads);
+    if (ids > INT32_MAX / 2) return PD_ERR_UNSUPPORTED_SHAPE;
+    const int grid = static_cast<int>(ids < sm_count() ? ids : sm_count());
+    attn_prompt_kernel<D, BF16><<<grid, kThreads, PromptSmem<D>::kTotal, stream>>>(mq, mk, mv, a, static_cast<int>(ids));
     count_launch();
     return cuda_ok(cudaGetLastError());
 }
