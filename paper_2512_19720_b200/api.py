@@ -361,81 +361,97 @@ def pd_fit_layer(x_tr, y_tr, x_val, y_val, w_b, mask, v_row0, v_col0, epochs, ba
     return v_out, axis_out, val_loss
 
 
+# The attention calls are short (a few microseconds on the GPU), so that their binding looks at each tensor once.
 _attn_ws_cache: dict = {}
+_HALF_TYPES = (torch.float16, torch.bfloat16)
 
 
-def _attn_workspace(device, stream: int) -> torch.Tensor:
-    """The attention calls' own scratch tensor, one for each device and stream: it must be all zero before its first
-    call, and calls that overlap on the GPU must not share it."""
-    key = (device.index, stream)
-    ws = _attn_ws_cache.get(key)
+def _attn_workspace(index: int, stream: int):
+    """The attention calls' own scratch tensor with its address and size, one for each device and stream: it must be all
+    zero before its first call, and calls that overlap on the GPU must not share it."""
+    ws = _attn_ws_cache.get((index, stream))
     if ws is None:
-        ws = _attn_ws_cache[key] = torch.zeros(workspace_bytes(OP_ATTN), dtype=torch.uint8, device=device)
+        t = torch.zeros(workspace_bytes(OP_ATTN), dtype=torch.uint8, device=torch.device("cuda", index))
+        ws = _attn_ws_cache[index, stream] = (t, t.data_ptr(), t.numel())
     return ws
 
 
 def attn_workspace(device=None) -> torch.Tensor:
     """The workspace that attention calls without one of their own use on the current stream (for pd_device_status)."""
-    device = device or torch.device("cuda", torch.cuda.current_device())
-    return _attn_workspace(device, torch.cuda.current_stream(device).cuda_stream)
+    index = torch.cuda.current_device() if device is None or device.index is None else device.index
+    return _attn_workspace(index, torch._C._cuda_getCurrentRawStream(index))[0]
 
 
-def _heads(t, name, dtype=None, device=None):
-    """Checks an activation [tokens, heads, head_dim]; a stride over heads or tokens may be anything that the library takes."""
-    if t.dim() != 3 or not t.is_cuda or t.dtype != (dtype or t.dtype) or t.dtype not in (torch.float16, torch.bfloat16):
-        raise TypeError(f"{name} must be a CUDA tensor [tokens, heads, head_dim] of {dtype or 'float16 or bfloat16'}")
-    if t.stride(2) != 1:
-        raise ValueError(f"{name}: the values of a head must be contiguous")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, other tensors on {device}")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+def _heads(t, name, dtype, index):
+    """Address and strides of an activation [tokens, heads, head_dim]; the library checks the strides."""
+    strides = t.stride()
+    if t.dtype is not dtype or dtype not in _HALF_TYPES or t.get_device() != index or index < 0:
+        raise TypeError(f"{name} must be a tensor of {dtype if dtype in _HALF_TYPES else 'float16 or bfloat16'} on CUDA device {index}: got {t.dtype} on {t.device}")
+    if len(strides) != 3 or strides[2] != 1:
+        raise ValueError(f"{name}: [tokens, heads, head_dim] with contiguous heads is wanted: got shape {tuple(t.shape)}, strides {strides}")
+    return t.data_ptr(), strides[0], strides[1]
 
 
-def _index(t, name, shape, device):
-    if t.dtype != torch.int32 or t.device != device:
-        raise TypeError(f"{name} must be an int32 tensor on {device}")
-    if t.dim() != len(shape) or any(want is not None and got != want for got, want in zip(t.shape, shape)) or t.stride(-1) != 1:
-        raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit, or is not contiguous")
+def _flat(t, name, dtype, index, shape):
+    """Address of a contiguous tensor of a shape."""
+    if t.dtype is not dtype or t.get_device() != index:
+        raise TypeError(f"{name} must be a tensor of {dtype} on CUDA device {index}: got {t.dtype} on {t.device}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor {tuple(shape)} is wanted: got shape {tuple(t.shape)}, strides {t.stride()}")
     return t.data_ptr()
 
 
-def _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, device):
-    for t, name, dtype, ndim in ((k_codes, "k_codes", torch.int8, 4), (v_codes, "v_codes", torch.int8, 4), (k_scale, "k_scale", torch.float32, 2),
-                                 (v_scale, "v_scale", torch.float32, 2)):
-        if t.dtype != dtype or t.device != device:
-            raise TypeError(f"{name} must be a tensor of {dtype} on {device}")
-        if t.dim() != ndim or t.shape[:2] != k_codes.shape[:2] or not t.is_contiguous():
-            raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit, or is not contiguous")
-    if k_codes.shape != v_codes.shape or k_codes.shape[1] != kv_heads or k_codes.shape[3] != head_dim:
-        raise ValueError(f"the cache holds {tuple(k_codes.shape)} codes [pages, kv_heads, page, head_dim], the call has {kv_heads} heads of {head_dim}")
-    return k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_codes.shape[0], k_codes.shape[2]
+def _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index):
+    shape = k_codes.shape
+    if len(shape) != 4 or (kv_heads is not None and shape[1] != kv_heads) or shape[3] != head_dim:
+        raise ValueError(f"k_codes: [pages, kv_heads, page, head_dim] is wanted with {'any' if kv_heads is None else kv_heads} heads of {head_dim}: got {tuple(shape)}")
+    return (_flat(k_codes, "k_codes", torch.int8, index, shape), _flat(v_codes, "v_codes", torch.int8, index, shape),
+            _flat(k_scale, "k_scale", torch.float32, index, shape[:2]), _flat(v_scale, "v_scale", torch.float32, index, shape[:2]), shape[0], shape[2])
 
 
-def _attn_call(name, bf16, device, args, workspace):
-    """Calls entry point `name` with `args`, a workspace and the current stream of `device`."""
-    with torch.cuda.device(device):
-        stream = torch.cuda.current_stream(device).cuda_stream
-        ws = workspace if workspace is not None else _attn_workspace(device, stream)
-        _check(getattr(lib, name + "_bf16" if bf16 else name)(*args, ws.data_ptr(), ws.numel() * ws.element_size(), stream), name)
+def _table(seq_lens, block_table, n_seqs, index):
+    shape, strides = block_table.shape, block_table.stride()
+    if block_table.dtype is not torch.int32 or block_table.get_device() != index:
+        raise TypeError(f"block_table must be an int32 tensor on CUDA device {index}: got {block_table.dtype} on {block_table.device}")
+    if len(shape) != 2 or shape[0] != n_seqs or (strides[1] != 1 and shape[1] > 1):
+        raise ValueError(f"block_table: [{n_seqs}, pages of a sequence] with contiguous rows is wanted: got shape {tuple(shape)}, strides {strides}")
+    width = shape[1]
+    return _flat(seq_lens, "seq_lens", torch.int32, index, (n_seqs,)), block_table.data_ptr(), strides[0] if n_seqs > 1 else width, width
+
+
+def _attn_call(name, fn, index, args, workspace):
+    """Calls an entry point with `args`, a workspace and the current stream of device `index`."""
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return _attn_call(name, fn, index, args, workspace)
+    stream = torch._C._cuda_getCurrentRawStream(index)  # current_stream().cuda_stream without the Python object: 2 us less a call
+    if workspace is None:
+        _, ptr, size = _attn_workspace(index, stream)
+    else:
+        ptr, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    code = fn(*args, ptr, size, stream)
+    if code:
+        raise PdError(code, name)
 
 
 def pd_attn_prompt(q, k, v, cu_seqlens, scale=None, out=None, workspace=None):
     """Causal attention over packed prompts: q [T, q_heads, head_dim], k and v [T, kv_heads, head_dim], cu_seqlens int32
     [n_seqs + 1]; scale: 1 / sqrt(head_dim) unless given.  Returns out [T, q_heads, head_dim]."""
-    n_tokens, q_heads, head_dim = q.shape if q.dim() == 3 else (0, 0, 0)
-    dev = q.device
-    views = _heads(q, "q") + _heads(k, "k", q.dtype, dev) + _heads(v, "v", q.dtype, dev)
-    if k.shape != v.shape or k.shape[0] != n_tokens or k.shape[2] != head_dim:
-        raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
-    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+    dtype, index, shape, kv_shape = q.dtype, q.get_device(), q.shape, k.shape
+    views = _heads(q, "q", dtype, index) + _heads(k, "k", dtype, index) + _heads(v, "v", dtype, index)
+    n_tokens, q_heads, head_dim = shape
+    if kv_shape != v.shape or kv_shape[0] != n_tokens or kv_shape[2] != head_dim:
+        raise ValueError(f"shapes do not fit: q {tuple(shape)}, k {tuple(kv_shape)}, v {tuple(v.shape)}")
+    n_seqs = cu_seqlens.numel() - 1
+    if n_seqs < 1:
         raise ValueError("cu_seqlens: one offset more than there are sequences is wanted")
     if out is None:
-        out = torch.empty((n_tokens, q_heads, head_dim), dtype=q.dtype, device=dev)
-    elif out.shape != q.shape:
-        raise ValueError(f"out: shape {tuple(out.shape)}, wanted {tuple(q.shape)}")
-    args = views + (_index(cu_seqlens, "cu_seqlens", (None,), dev), cu_seqlens.numel() - 1, n_tokens, q_heads, k.shape[1], head_dim,
-                    head_dim ** -0.5 if scale is None else scale) + _heads(out, "out", q.dtype, dev)
-    _attn_call("pd_attn_prompt", q.dtype == torch.bfloat16, dev, args, workspace)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != shape:
+        raise ValueError(f"out: shape {tuple(out.shape)}, wanted {tuple(shape)}")
+    args = views + (_flat(cu_seqlens, "cu_seqlens", torch.int32, index, (n_seqs + 1,)), n_seqs, n_tokens, q_heads, kv_shape[1], head_dim,
+                    head_dim ** -0.5 if scale is None else scale) + _heads(out, "out", dtype, index)
+    _attn_call("pd_attn_prompt", lib.pd_attn_prompt_bf16 if dtype is torch.bfloat16 else lib.pd_attn_prompt, index, args, workspace)
     return out
 
 
@@ -444,40 +460,32 @@ def pd_kv_append(k, v, k_codes, v_codes, k_scale, v_scale, cu_seqlens, seq_lens,
     int8 [n_pages, kv_heads, page, head_dim], scales fp32 [n_pages, kv_heads].  seq_lens int32 [n_seqs]: lengths AFTER the
     call; block_table int32 [n_seqs, width].  k_values, v_values [T, kv_heads, head_dim], dense, take the values that the new
     codes stand for (may be k and v)."""
-    n_tokens, kv_heads, head_dim = k.shape if k.dim() == 3 else (0, 0, 0)
-    dev = k.device
-    views = _heads(k, "k") + _heads(v, "v", k.dtype, dev)
-    if k.shape != v.shape:
-        raise ValueError(f"shapes do not fit: k {tuple(k.shape)}, v {tuple(v.shape)}")
-    for t, name in ((k_values, "k_values"), (v_values, "v_values")):
-        if t is not None:
-            _heads(t, name, k.dtype, dev)
-            if t.shape != k.shape or not t.is_contiguous():
-                raise ValueError(f"{name}: a dense tensor {tuple(k.shape)} is wanted")
+    dtype, index, shape = k.dtype, k.get_device(), k.shape
+    views = _heads(k, "k", dtype, index) + _heads(v, "v", dtype, index)
+    if shape != v.shape:
+        raise ValueError(f"shapes do not fit: k {tuple(shape)}, v {tuple(v.shape)}")
+    n_tokens, kv_heads, head_dim = shape
     n_seqs = seq_lens.numel()
-    codes = _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, dev)
-    args = views + (_index(cu_seqlens, "cu_seqlens", (n_seqs + 1,), dev), n_seqs, n_tokens, kv_heads, head_dim) + codes + (
-        _index(seq_lens, "seq_lens", (None,), dev), _index(block_table, "block_table", (n_seqs, None), dev), block_table.stride(0) if n_seqs > 1 else
-        block_table.shape[1], block_table.shape[1], _ptr(k_values), _ptr(v_values))
-    _attn_call("pd_kv_append", k.dtype == torch.bfloat16, dev, args, workspace)
+    args = views + (_flat(cu_seqlens, "cu_seqlens", torch.int32, index, (n_seqs + 1,)), n_seqs, n_tokens, kv_heads, head_dim) + _cache(
+        k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index) + _table(seq_lens, block_table, n_seqs, index) + (
+        None if k_values is None else _flat(k_values, "k_values", dtype, index, shape), None if v_values is None else _flat(v_values, "v_values", dtype, index, shape))
+    _attn_call("pd_kv_append", lib.pd_kv_append_bf16 if dtype is torch.bfloat16 else lib.pd_kv_append, index, args, workspace)
 
 
 def pd_attn_cache(q, k_codes, v_codes, k_scale, v_scale, seq_lens, block_table, scale=None, out=None, workspace=None):
     """Attention of one token per sequence, q [n_seqs, q_heads, head_dim], over the first seq_lens[b] tokens of its pages
     (the cache of pd_kv_append).  Returns out [n_seqs, q_heads, head_dim]; zeros for an empty sequence."""
-    n_seqs, q_heads, head_dim = q.shape if q.dim() == 3 else (0, 0, 0)
-    dev = q.device
-    view = _heads(q, "q")
-    kv_heads = k_codes.shape[1] if k_codes.dim() == 4 else 0
+    dtype, index, shape = q.dtype, q.get_device(), q.shape
+    view = _heads(q, "q", dtype, index)
+    n_seqs, q_heads, head_dim = shape
     if out is None:
-        out = torch.empty((n_seqs, q_heads, head_dim), dtype=q.dtype, device=dev)
-    elif out.shape != q.shape:
-        raise ValueError(f"out: shape {tuple(out.shape)}, wanted {tuple(q.shape)}")
-    codes = _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, dev)
-    args = view + (n_seqs, q_heads, kv_heads, head_dim, head_dim ** -0.5 if scale is None else scale) + codes + (
-        _index(seq_lens, "seq_lens", (n_seqs,), dev), _index(block_table, "block_table", (n_seqs, None), dev),
-        block_table.stride(0) if n_seqs > 1 else block_table.shape[1], block_table.shape[1]) + _heads(out, "out", q.dtype, dev)
-    _attn_call("pd_attn_cache", q.dtype == torch.bfloat16, dev, args, workspace)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != shape:
+        raise ValueError(f"out: shape {tuple(out.shape)}, wanted {tuple(shape)}")
+    codes = _cache(k_codes, v_codes, k_scale, v_scale, None, head_dim, index)
+    args = view + (n_seqs, q_heads, k_codes.shape[1], head_dim, head_dim ** -0.5 if scale is None else scale) + codes + _table(
+        seq_lens, block_table, n_seqs, index) + _heads(out, "out", dtype, index)
+    _attn_call("pd_attn_cache", lib.pd_attn_cache_bf16 if dtype is torch.bfloat16 else lib.pd_attn_cache, index, args, workspace)
     return out
 
 
