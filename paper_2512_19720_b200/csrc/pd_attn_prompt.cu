@@ -9,17 +9,20 @@
 // 128 x 128 scores is 1024 clocks of products at head_dim 128 and 1024 clocks of the 16 exponentials a clock that an SM has.
 //
 // A block works on units of two *slots* of 128 queries each that read the same keys: two heads that share their key/value
-// head where their number is even, else two consecutive pieces of one head's queries.  While one slot's scores are in the
-// softmax the tensor cores work for the other.  Tiles of 128 keys: S = Q K^T (both operands in shared memory) into tensor
-// memory, softmax by one thread per row, P back into tensor memory in S's place, O += P V with P from tensor memory.  P is
-// handed over in two halves, so that the second product starts while the second half's exponentials are computed.
-// Tensor memory is full: 2 x 128 columns of S (P inside), 2 x 128 of O.
+// head where their number is even, else two consecutive pieces of one head's queries.  Tiles of 128 keys: S = Q K^T (both
+// operands in shared memory) into tensor memory, softmax by one thread per row, P into tensor memory, O += P V with P from
+// tensor memory.  P is handed over in two halves, so that the second product starts while the other half's exponentials
+// are computed.
+// Tensor memory: one buffer of 128 columns for S that both slots use in turn (a row of S is taken into registers at once, and
+// the buffer is free again long before its softmax is done), 64 columns of P and 128 of O for each slot.  So the scores of a
+// slot's next tile wait for its softmax, not the softmax for them.  With a buffer of S for each slot and P in its place, a
+// slot's softmax stood still during its own two products: 64 query heads, 8192 tokens 1110 us.
 //
-// Roles: warps 0-3 and 4-7 the softmax and the output of slot 0 and 1; warp 8 units and TMA; warp 9 issues the products;
-// warps 10 and 11 look for infinities and NaN among the values of the tile on the diagonal, where 0 * v must not reach the
-// queries that do not attend to v: they are set to zero there, and the output adds them for the queries that do.
-// The products of a block are issued by one thread and run in the order of issue: S of the next tile follows the product
-// that reads P from the same place.  Every wait is bounded.
+// Roles: warps 0-3 and 4-7 the softmax and the output of slot 0 and 1; warp 8 units and TMA; warps 9 and 10 issue the
+// products with the keys and with the values (one warp for both was kept from one by its waits for the other); warp 11
+// looks for infinities and NaN among the values of a tile on the diagonal, where 0 * v must not reach the
+// queries that do not attend to v: they are set to zero there, and the output adds them for the queries that do.  A tile on
+// the diagonal is full for the products when it has been through it.  Every wait is bounded.
 #include "pd_attn.cuh"
 #include "pd_tcgen05.cuh"
 
@@ -32,7 +35,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kUnits = 4;  // units that the producer may be ahead
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLead = 8.f;  // how far (base-2 exponent) a score may pass the reference maximum
-constexpr uint32_t kColS = 0, kColO = 256;  // tensor-memory columns; slot 1: + 128
+constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;  // tensor-memory columns; slot 1: P + 64, O + 128
 
 struct Unit {
     int first, len;  // the sequence's first token and its length; len 0: no more units
@@ -51,22 +54,23 @@ struct Slots {
 template <int D>
 struct PromptSmem {
     static constexpr int kTileBytes = kTile * D * 2;
-    static constexpr int kStages = D == 128 ? 5 : 8;  // of keys or values
+    static constexpr int kStages = D == 128 ? 4 : 8;  // of keys or values
     static constexpr int kQ = 0;
     static constexpr int kRing = 2 * kTileBytes;
-    static constexpr int kBars = kRing + kStages * kTileBytes;
+    static constexpr int kOut = kRing + kStages * kTileBytes;  // for each softmax warp 32 rows of 64 outputs
+    static constexpr int kBars = kOut + 8 * 32 * 128;
     static constexpr int kTotal = kBars + 1024 + 1024;  // + slack for 1024-byte alignment
     static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
 struct Bars {
     uint64_t kv_full[8], kv_empty[8];
+    uint64_t v_landed[4];  // tiles on a diagonal, in turn: no more of them are in the ring
     uint64_t q_full[2], q_empty[2];
-    uint64_t s_full[2], p_half[2][2], o_done[2], o_empty[2];
-    uint64_t v_ask, v_clean;  // a tile on a diagonal has landed, has been looked through
+    uint64_t s_full[2], s_free, p_half[2][2], o_done[2], o_empty[2];
     uint64_t unit_full[kUnits], unit_empty[kUnits];
     Unit units[kUnits];
-    int taint[kUnits][2];
+    int taint[kUnits];
     uint32_t tmem;
     int abort_flag;
 };
@@ -98,25 +102,53 @@ __device__ __forceinline__ bool non_finite2(uint32_t w) {
     return (w & e) == e || ((w >> 16) & e) == e;
 }
 
-// A and B in shared memory
+// The products and their commits are written for a whole warp of which one elected thread acts: inside `if (lane == 0)` the
+// compiler moved every operand of every instruction to the uniform registers anew, and the issue of a 64-clock product took
+// 105 clocks.
 __device__ __forceinline__ void mma_smem_a(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n"
-        ".reg .pred p;\n"
+        ".reg .pred p, q;\n"
         "setp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "elect.sync _|q, 0xffffffff;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
         "}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// B operand with the head dimension contiguous (the contraction runs over rows of 128 bytes): groups of 8 rows 1024 bytes
-// apart, pieces of 64 columns a whole sub-tile apart; 128-byte swizzle
-__device__ __forceinline__ uint64_t make_v_desc(uint32_t addr, uint32_t piece_bytes) {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((addr & 0x3FFFFu) >> 4);
-    d |= static_cast<uint64_t>(piece_bytes >> 4) << 16;
-    d |= static_cast<uint64_t>(1024 >> 4) << 32;
-    d |= static_cast<uint64_t>(1) << 46;
-    d |= static_cast<uint64_t>(2) << 61;
+__device__ __forceinline__ void mma_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "elect.sync _|q, 0xffffffff;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+        "}\n" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_elected(uint64_t *bar) {
+    asm volatile(
+        "{\n"
+        ".reg .pred q;\n"
+        "elect.sync _|q, 0xffffffff;\n"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n"
+        "}\n" ::"r"(smem_u32(bar))
+        : "memory");
+}
+// Matrix descriptors of operands in rows of 128 bytes with the 128-byte swizzle, groups of 8 rows 1024 bytes apart.  Upper
+// half: that distance, the descriptor's version, the swizzle.  Lower half: address; for a B operand whose contraction
+// runs over the rows also the distance between its pieces of 64 columns (unused otherwise).
+__device__ __forceinline__ uint64_t make_desc(uint32_t lower) {
+    constexpr uint32_t upper = (1024u >> 4) | (1u << 14) | (2u << 29);
+    return (static_cast<uint64_t>(upper) << 32) | lower;
+}
+__device__ __forceinline__ uint32_t desc_lower(const void *p, uint32_t piece_bytes) { return (smem_u32(p) >> 4) | ((piece_bytes >> 4) << 16); }
+
+// acc stays zero unless one of the 16-bit values is an infinity or a NaN
+template <bool BF16>
+__device__ __forceinline__ uint32_t times_zero(uint32_t w, uint32_t acc) {
+    uint32_t d;
+    if (BF16) asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(w), "r"(0u), "r"(acc));
+    else asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(w), "r"(0u), "r"(acc));
     return d;
 }
 
@@ -127,6 +159,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     using E = Elem<BF16>;
     using L = PromptSmem<D>;
     constexpr int kStages = L::kStages;
+    static_assert(kStages % 2 == 0, "keys and values keep to their own stages");
     constexpr int kPieces = D / 64;                    // sub-tiles of 64 columns
     constexpr int kPieceBytes = kTile * 64 * 2;
     extern __shared__ unsigned char smem_raw[];
@@ -141,11 +174,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) mbar_init(bar.kv_full + i, 1), mbar_init(bar.kv_empty + i, 1);
+        for (int i = 0; i < 4; ++i) mbar_init(bar.v_landed + i, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(bar.q_full + s, 1), mbar_init(bar.q_empty + s, 1), mbar_init(bar.s_full + s, 1);
             mbar_init(bar.p_half[s], 4), mbar_init(bar.p_half[s] + 1, 4), mbar_init(bar.o_done + s, 1), mbar_init(bar.o_empty + s, 4);
         }
-        mbar_init(&bar.v_ask, 1), mbar_init(&bar.v_clean, 2);
+        mbar_init(&bar.s_free, 4);
         for (int i = 0; i < kUnits; ++i) mbar_init(bar.unit_full + i, 1), mbar_init(bar.unit_empty + i, 11);
         bar.abort_flag = 0;
         mbar_fence_init();
@@ -170,14 +204,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     };
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         if (warp == 8) {
             // -------------------------------------------------------- units and TMA
             // Sequence b's units are the ids from (cu[b] / span + b) * per_tile on, `span` queries to a unit: never more of them
             // than ids before the next sequence's.  Ids that no unit has are passed over.
             const int span = slots.by_head ? kTile : 2 * kTile;
             const int per_tile = slots.by_head ? a.q_heads / 2 : a.q_heads;
-            uint32_t it = 0, n_q[2] = {0, 0};
+            uint32_t it = 0, n_diag = 0, n_q[2] = {0, 0};
             bool ok = true;
             int id = lane == 0 ? static_cast<int>(atomicAdd(a.counters, 1u)) : 0;
             while (ok) {
@@ -220,143 +254,152 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ++n_unit;
                 if (end_mark) break;
                 if (lane == 0) {
-                    const int n = slots.max_tiles(u), kvh = u.head / group;
+                    const int n0 = slots.tiles(u, 0), n = slots.max_tiles(u), kvh = u.head / group;
                     auto load = [&](const CUtensorMap *map, unsigned char *dst, uint64_t *full, int head, int row) {
                         mbar_arrive_expect_tx(full, L::kTileBytes);
 #pragma unroll
                         for (int p = 0; p < kPieces; ++p) tma_load_3d(map, full, dst + p * kPieceBytes, p * 64, head, row);
                     };
                     for (int j = 0; j < n && ok; ++j) {
-                        if (j == 0) {
-                            for (int s = 0; s < 2 && ok; ++s) {
-                                if (slots.tiles(u, s) == 0) continue;
-                                if (n_q[s] > 0 && !(ok = wait(bar.q_empty + s, n_q[s] - 1, 52))) break;
-                                ++n_q[s];
-                                load(&map_q, smem + L::kQ + s * L::kTileBytes, bar.q_full + s, slots.head(u, s), u.first + slots.q0(u, s));
-                            }
-                        }
                         for (int kv = 0; kv < 2 && ok; ++kv, ++it) {
                             const uint32_t st = it % kStages, round = it / kStages;
                             if (round > 0 && !(ok = wait(bar.kv_empty + st, round - 1, 53))) break;
-                            load(kv == 0 ? &map_k : &map_v, smem + L::kRing + st * L::kTileBytes, bar.kv_full + st, kvh, u.first + j * kTile);
+                            uint64_t *full = bar.kv_full + st;
+                            if (kv == 1 && j >= n0 - 1) full = bar.v_landed + n_diag++ % 4;  // on a diagonal: warp 11 first
+                            load(kv == 0 ? &map_k : &map_v, smem + L::kRing + st * L::kTileBytes, full, kvh, u.first + j * kTile);
+                            if (j == 0 && kv == 0) {
+#pragma unroll
+                                for (int s = 0; s < 2; ++s) {
+                                    if (!ok || slots.tiles(u, s) == 0) continue;
+                                    if (n_q[s] > 0 && !(ok = wait(bar.q_empty + s, n_q[s] - 1, 52))) continue;
+                                    ++n_q[s];
+                                    load(&map_q, smem + L::kQ + s * L::kTileBytes, bar.q_full + s, slots.head(u, s), u.first + slots.q0(u, s));
+                                }
+                            }
                         }
                     }
                 }
                 ok = __all_sync(0xffffffffu, ok);
             }
         } else if (warp == 9) {
-            // -------------------------------------------------------- the products, issued by one thread
-            constexpr uint32_t kIdescS = kIdescBase<BF16> | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
-            constexpr uint32_t kIdescO = kIdescBase<BF16> | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
-            uint32_t it = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0}, n_clean = 0;
+            // -------------------------------------------------------- S = Q K^T of the units' steps: their slots' tiles in turn
+            constexpr uint32_t kIdesc = kIdescBase<BF16> | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+            const uint32_t q_desc = desc_lower(smem + L::kQ, 16), k_desc = desc_lower(smem + L::kRing, 16);
+            uint32_t it = 0, n_step = 0, n_q[2] = {0, 0};
             bool ok = true;
             Unit u;
             while (ok && next_unit(u)) {
+                // the same in all lanes, which the compiler then knows
+                u.len = __shfl_sync(0xffffffffu, u.len, 0), u.q0 = __shfl_sync(0xffffffffu, u.q0, 0);
                 const int n0 = slots.tiles(u, 0), n1 = slots.tiles(u, 1), n = max(n0, n1);
-                if (lane == 0) {
-                    auto scores = [&](int s, int j) {  // S = Q K_j^T
-                        const uint32_t q = smem_u32(smem + L::kQ + s * L::kTileBytes);
-                        const uint32_t k = smem_u32(smem + L::kRing + ((it + 2 * j) % kStages) * L::kTileBytes);
+                for (int j = 0; j < n && ok; ++j, it += 2) {
+                    const uint32_t st = it % kStages;
+                    if (!(ok = wait_warp(bar.kv_full + st, it / kStages, 54))) break;
+                    const uint32_t k = k_desc + st * (L::kTileBytes >> 4);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int ns = s ? n1 : n0;
+                        if (!ok || j >= ns) continue;
+                        if (j == 0 && !(ok = wait_warp(bar.q_full + s, n_q[s]++, 55))) continue;
+                        if (n_step > 0 && !(ok = wait_warp(&bar.s_free, n_step - 1, 56))) continue;
+                        ++n_step;
+                        tcgen05_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
-                            const uint32_t off = (kk / 4) * kPieceBytes + (kk % 4) * 32;
-                            mma_smem_a(tmem + kColS + s * 128, make_smem_desc(q + off), make_smem_desc(k + off), kIdescS, kk > 0);
+                            const uint32_t off = ((kk / 4) * kPieceBytes + (kk % 4) * 32) >> 4;
+                            mma_smem_a(tmem + kColS, make_desc(q_desc + s * (L::kTileBytes >> 4) + off), make_desc(k + off), kIdesc, kk > 0);
                         }
-                        tcgen05_commit(bar.s_full + s);
-                    };
-                    auto full = [&](int i) { return wait(bar.kv_full + (it + i) % kStages, (it + i) / kStages, 54); };
-                    ok = full(0);
-                    for (int s = 0; s < 2 && ok; ++s) {
-                        if ((s ? n1 : n0) == 0) continue;
-                        if (!(ok = wait(bar.q_full + s, n_q[s], 55))) break;
-                        ++n_q[s];
-                        tcgen05_fence_after();
-                        scores(s, 0);
-                        if ((s ? n1 : n0) == 1) tcgen05_commit(bar.q_empty + s);
+                        commit_elected(bar.s_full + s);
+                        if (j + 1 == ns) commit_elected(bar.q_empty + s);
                     }
-                    if (ok) tcgen05_commit(bar.kv_empty + it % kStages);
-                    for (int j = 0; j < n && ok; ++j) {
-                        if (!(ok = full(2 * j + 1))) break;
-                        const bool diagonal = j == n0 - 1 || j == n1 - 1;
-                        if (diagonal) {
-                            mbar_arrive(&bar.v_ask);
-                            if (!(ok = wait(&bar.v_clean, n_clean++, 56))) break;
-                        }
-                        if (j + 1 < n && !(ok = full(2 * j + 2))) break;
-                        const uint32_t v = smem_u32(smem + L::kRing + ((it + 2 * j + 1) % kStages) * L::kTileBytes);
-                        for (int s = 0; s < 2 && ok; ++s) {
-                            const int ns = s ? n1 : n0;
-                            if (j >= ns) continue;
-                            if (j == 0 && n_q[s] > 1 && !(ok = wait(bar.o_empty + s, n_q[s] - 2, 57))) break;
-#pragma unroll
-                            for (int half = 0; half < 2 && ok; ++half) {
-                                if (!(ok = wait(bar.p_half[s] + half, n_p[s], 58))) break;
-                                tcgen05_fence_after();
-#pragma unroll
-                                for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
-                                    tcgen05_mma_f16_tmem_a(tmem + kColO + s * 128, tmem + kColS + s * 128 + kk * 8, make_v_desc(v + kk * 2048, kPieceBytes),
-                                                           kIdescO, (j > 0 || kk > 0) ? 1u : 0u);
-                            }
-                            if (!ok) break;
-                            ++n_p[s];
-                            tcgen05_commit(bar.o_done + s);
-                            if (j + 1 < ns) {
-                                scores(s, j + 1);
-                                if (j + 2 == ns) tcgen05_commit(bar.q_empty + s);
-                            }
-                        }
-                        if (!ok) break;
-                        tcgen05_commit(bar.kv_empty + (it + 2 * j + 1) % kStages);
-                        if (j + 1 < n) tcgen05_commit(bar.kv_empty + (it + 2 * j + 2) % kStages);
-                    }
+                    if (ok) commit_elected(bar.kv_empty + st);
                 }
                 ok = __all_sync(0xffffffffu, ok);
-                it += 2 * n;
+                done_unit();
+            }
+        } else if (warp == 10) {
+            // -------------------------------------------------------- O += P V of the same steps
+            constexpr uint32_t kIdesc = kIdescBase<BF16> | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+            const uint32_t v_desc = desc_lower(smem + L::kRing, kPieceBytes);
+            uint32_t it = 0, n_u[2] = {0, 0}, n_p[2] = {0, 0};
+            bool ok = true;
+            Unit u;
+            while (ok && next_unit(u)) {
+                u.len = __shfl_sync(0xffffffffu, u.len, 0), u.q0 = __shfl_sync(0xffffffffu, u.q0, 0);
+                const int n0 = slots.tiles(u, 0), n1 = slots.tiles(u, 1), n = max(n0, n1);
+                for (int j = 0; j < n && ok; ++j, it += 2) {
+                    const uint32_t st = (it + 1) % kStages;
+                    if (!(ok = wait_warp(bar.kv_full + st, (it + 1) / kStages, 57))) break;
+                    const uint32_t v = v_desc + st * (L::kTileBytes >> 4);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        if (!ok || j >= (s ? n1 : n0)) continue;
+                        if (j == 0 && n_u[s]++ > 0 && !(ok = wait_warp(bar.o_empty + s, n_u[s] - 2, 58))) continue;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (!ok || !(ok = wait_warp(bar.p_half[s] + half, n_p[s], 60))) continue;
+                            tcgen05_fence_after();
+#pragma unroll
+                            for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
+                                mma_tmem_a(tmem + kColO + s * 128, tmem + kColP + s * 64 + kk * 8, make_desc(v + kk * (2048 >> 4)), kIdesc, (j > 0 || kk > 0) ? 1u : 0u);
+                        }
+                        if (!ok) continue;
+                        ++n_p[s];
+                        commit_elected(bar.o_done + s);
+                    }
+                    if (ok) commit_elected(bar.kv_empty + st);
+                }
+                ok = __all_sync(0xffffffffu, ok);
                 done_unit();
             }
         } else {
             // -------------------------------------------------------- values on the diagonal: no infinities and NaN in shared memory
-            uint32_t it = 0, n_ask = 0;
+            uint32_t it = 0, n_diag = 0;
             bool ok = true;
             Unit u;
             while (ok && next_unit(u)) {
                 const int n0 = slots.tiles(u, 0), n1 = slots.tiles(u, 1), n = max(n0, n1);
                 bool found = false;
-                for (int j = n0 - 1; j < n && ok; ++j) {
-                    const uint32_t i = it + 2 * j + 1;
-                    if (!(ok = wait_warp(&bar.v_ask, n_ask++, 59))) break;
-                    uint4 *p = reinterpret_cast<uint4 *>(smem + L::kRing + (i % kStages) * L::kTileBytes) + (warp - 10) * 32 + lane;
+                for (int j = n0 - 1; j < n; ++j, ++n_diag) {
+                    const uint32_t st = (it + 2 * j + 1) % kStages;
+                    if (!(ok = wait_warp(bar.v_landed + n_diag % 4, n_diag / 4, 59))) break;
+                    uint4 *p = reinterpret_cast<uint4 *>(smem + L::kRing + st * L::kTileBytes) + lane;
+                    uint32_t acc[4] = {0u, 0u, 0u, 0u};
 #pragma unroll 8
-                    for (int k = 0; k < L::kTileBytes / 16 / 64; ++k) {
-                        uint4 x = p[k * 64];
-                        if (non_finite2<BF16>(x.x) || non_finite2<BF16>(x.y) || non_finite2<BF16>(x.z) || non_finite2<BF16>(x.w)) {
-                            found = true;
+                    for (int k = 0; k < L::kTileBytes / 16 / 32; ++k) {
+                        const uint4 x = p[k * 32];
+                        acc[0] = times_zero<BF16>(x.x, acc[0]), acc[1] = times_zero<BF16>(x.y, acc[1]);
+                        acc[2] = times_zero<BF16>(x.z, acc[2]), acc[3] = times_zero<BF16>(x.w, acc[3]);
+                    }
+                    if (__any_sync(0xffffffffu, ((acc[0] | acc[1] | acc[2] | acc[3]) & 0x7fff7fffu) != 0u)) {
+                        found = true;
+                        for (int k = 0; k < L::kTileBytes / 16 / 32; ++k) {
+                            const uint4 x = p[k * 32];
                             uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 if (non_finite2<BF16>(w[c] & 0xffffu)) w[c] &= 0xffff0000u;
                                 if (non_finite2<BF16>(w[c] & 0xffff0000u)) w[c] &= 0xffffu;
                             }
-                            p[k * 64] = make_uint4(w[0], w[1], w[2], w[3]);
+                            p[k * 32] = make_uint4(w[0], w[1], w[2], w[3]);
                         }
+                        fence_proxy_async_smem();
                     }
-                    found = __any_sync(0xffffffffu, found);
-                    if (lane == 0) bar.taint[n_unit % kUnits][warp - 10] = found;
-                    fence_proxy_async_smem();
+                    if (lane == 0) bar.taint[n_unit % kUnits] = found;
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&bar.v_clean);
+                    if (lane == 0) mbar_arrive(bar.kv_full + st);
                 }
                 it += 2 * n;
                 done_unit();
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // ------------------------------------------------------------ softmax and output: a thread owns one row of a slot
         const int s = warp >> 2;
         const int r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-        const uint32_t ts = lanes + kColS + s * 128, to = lanes + kColO + s * 128;
+        const uint32_t ts = lanes + kColS, tp = lanes + kColP + s * 64, to = lanes + kColO + s * 128;
         const float scale2 = a.scale * kLog2e;
         const float f = scale2 > 0.f ? scale2 : (scale2 < 0.f ? -scale2 : 1.f);
         uint32_t n_s = 0;
@@ -377,6 +420,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tcgen05_ld_32x32b_x32(ts + 32 * c, x[c]);
                 tcgen05_wait_ld();
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar.s_free);
                 if (scale2 <= 0.f) {  // the maximum is taken before the scores are scaled by |scale|
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -399,14 +445,17 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     top[c] = fmaxf(top[c], __uint_as_float(x[c][31]));
                 }
                 const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * f;
+                // the product with the tile before has been done: O may be rescaled, P written
+                if (j > 0) {
+                    if (!(ok = wait_warp(bar.o_done + s, n_s - 1, 61))) break;
+                    tcgen05_fence_after();
+                }
                 if (__any_sync(0xffffffffu, best > m + kMaxLead)) {
                     const float now = fmaxf(m, best), mu_new = now == -INFINITY ? 0.f : now;
                     const float shrink = exp2_approx(m - mu_new);  // 0 from -infinity on
                     m = now, mu = mu_new;
                     l.x *= shrink, l.y *= shrink;
-                    if (j > 0) {  // O of the tiles so far is complete, and the next product waits for this warp
-                        if (!(ok = wait_warp(bar.o_done + s, n_s - 1, 61))) break;
-                        tcgen05_fence_after();
+                    if (j > 0) {
 #pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
                             uint32_t o[32];
@@ -431,7 +480,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         l = add2(l, e);
                         p[k] = E::from_float2(e.x, e.y);
                     }
-                    tcgen05_st_32x32b_x32(ts + 32 * half, p);
+                    tcgen05_st_32x32b_x32(tp + 32 * half, p);
                     tcgen05_wait_st();
                     tcgen05_fence_before();
                     __syncwarp();
@@ -444,19 +493,25 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             tcgen05_fence_after();
             l0 = l.x + l.y;
             const float inv = 1.f / l0;
-            const bool taint = bar.taint[n_unit % kUnits][0] | bar.taint[n_unit % kUnits][1];
+            const bool taint = bar.taint[n_unit % kUnits] != 0;
             const int head = slots.head(u, s);
-            uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row) * a.out.token_stride + head * a.out.head_stride;
+            const int row0 = slots.q0(u, s) + (warp & 3) * 32;  // the warp's first row
+            uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0) * a.out.token_stride + head * a.out.head_stride;
+            // rows go through shared memory, so that they leave in lines of 128 bytes: written by the threads that own them they
+            // were 32 pieces of 16 bytes an instruction
+            unsigned char *out = smem + L::kOut + warp * (32 * 128);
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                tcgen05_ld_32x32b_x32(to + c, o);
-                tcgen05_wait_ld();
-                if (row < u.len) {
+            for (int c = 0; c < D; c += 64) {
+                uint32_t w[32];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t o[32];
+                    tcgen05_ld_32x32b_x32(to + c + 32 * h, o);
+                    tcgen05_wait_ld();
 #pragma unroll
                     for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * inv);
-                    if (taint) {
-                        const uint16_t *v = static_cast<const uint16_t *>(a.v.ptr) + (head / group) * a.v.head_stride + c;
+                    if (taint && row < u.len) {
+                        const uint16_t *v = static_cast<const uint16_t *>(a.v.ptr) + (head / group) * a.v.head_stride + c + 32 * h;
                         for (int key = u.q0; key <= row; ++key)
 #pragma unroll
                             for (int k = 0; k < 32; ++k) {
@@ -465,17 +520,25 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             }
                     }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = E::from_float2(__uint_as_float(o[8 * k + 2 * i]), __uint_as_float(o[8 * k + 2 * i + 1]));
-                        *reinterpret_cast<uint4 *>(y + c + 8 * k) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
+                    for (int k = 0; k < 16; ++k) w[16 * h + k] = E::from_float2(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
                 }
+                if (c + 64 == D) {  // O has been read
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar.o_empty + s);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *reinterpret_cast<uint4 *>(out + lane * 128 + ((k ^ (lane & 7)) * 16)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int i = 4 * k + (lane >> 3), piece = lane & 7;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(out + i * 128 + ((piece ^ (i & 7)) * 16));
+                    if (row0 + i < u.len) *reinterpret_cast<uint4 *>(y + i * a.out.token_stride + c + 8 * piece) = x;
+                }
+                __syncwarp();
             }
-            tcgen05_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar.o_empty + s);
             done_unit();
         }
     }
