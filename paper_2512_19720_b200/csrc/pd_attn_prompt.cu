@@ -81,6 +81,11 @@ __device__ __forceinline__ float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 d;
     asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 x, x, y, z;\nmov.b64 {%0, %1}, x;\n}\n"
@@ -155,7 +160,7 @@ __device__ __forceinline__ uint32_t times_zero(uint32_t w, uint32_t acc) {
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                   const PromptArgs a, const int n_ids) {
+                   const PromptArgs a) {
     using E = Elem<BF16>;
     using L = PromptSmem<D>;
     constexpr int kStages = L::kStages;
@@ -185,9 +190,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         mbar_fence_init();
     }
     if (warp == 9) tcgen05_alloc(&bar.tmem, 512);
+    if (warp == 8 && lane < 3) prefetch_tensormap(lane == 0 ? &map_q : (lane == 1 ? &map_k : &map_v));
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // everything before touches no memory of the caller's
     const uint32_t tmem = bar.tmem;
 
     // The next unit, in the producer's order: every other role reads what the producer wrote.
@@ -207,44 +215,44 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         if (warp == 8) {
             // -------------------------------------------------------- units and TMA
-            // Sequence b's units are the ids from (cu[b] / span + b) * per_tile on, `span` queries to a unit: never more of them
-            // than ids before the next sequence's.  Ids that no unit has are passed over.
-            const int span = slots.by_head ? kTile : 2 * kTile;
-            const int per_tile = slots.by_head ? a.q_heads / 2 : a.q_heads;
+            // Units in the order of their work, most first, so that the blocks end together: the last queries of every sequence
+            // that has as many tiles as the longest, then the tile before those, and so on; all heads of a tile in a row.
+            // More than 32 sequences are taken 32 at a time.  A lane knows one sequence; ids only grow, so that the walk over
+            // groups and tiles goes forward only.
+            const int span = slots.by_head ? kTile : 2 * kTile;                     // queries of a unit
+            const int per_tile = slots.by_head ? a.q_heads / 2 : a.q_heads;         // units of a tile
+            int g0 = -32, first = 0, len = 0, tiles = 0, level = 0, level_base = 0, group_end = 0;
             uint32_t it = 0, n_diag = 0, n_q[2] = {0, 0};
             bool ok = true;
-            int id = lane == 0 ? static_cast<int>(atomicAdd(a.counters, 1u)) : 0;
+            int id = blockIdx.x;
             while (ok) {
                 id = __shfl_sync(0xffffffffu, id, 0);
+                while (id >= group_end && g0 < a.n_seqs) {
+                    g0 += 32;
+                    tiles = 0;
+                    if (g0 + lane < a.n_seqs) {
+                        first = __ldg(a.cu_seqlens + g0 + lane);
+                        const int end = __ldg(a.cu_seqlens + g0 + lane + 1);
+                        len = end - first;
+                        if (first < 0 || end < first || end > a.n_tokens) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(g0 + lane));
+                        else tiles = (len + span - 1) / span;
+                    }
+                    level_base = group_end;
+                    group_end += __reduce_add_sync(0xffffffffu, tiles) * per_tile;
+                    level = __reduce_max_sync(0xffffffffu, tiles) - 1;
+                }
                 Unit u = {0, 0, 0, 0};
-                if (id < n_ids) {
-                    const int tile_id = id / per_tile;
-                    // the last sequence whose ids start at or before this one: 32 candidates a step
-                    int lo = 0, n = a.n_seqs;  // the answer is in [lo, lo + n)
-                    while (n > 1) {
-                        const int step = (n + 31) / 32;
-                        const int b = lo + lane * step;
-                        const bool le = lane * step < n && min(max(__ldg(a.cu_seqlens + b), 0), a.n_tokens) / span + b <= tile_id;
-                        const unsigned m = __ballot_sync(0xffffffffu, le);
-                        const int last = m ? 31 - __clz(m) : 0;
-                        lo += last * step;
-                        n = min(step, n - last * step);
-                    }
-                    const int first = __ldg(a.cu_seqlens + lo), end = __ldg(a.cu_seqlens + lo + 1);
-                    if (first < 0 || end < first || end > a.n_tokens) {
-                        if (lane == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(lo));
-                    } else {
-                        const int n_tiles = (end - first + span - 1) / span, k = tile_id - (first / span + lo);
-                        if (k >= 0 && k < n_tiles)  // the last queries first: theirs is the most work
-                            u = {first, end - first, (n_tiles - 1 - k) * span, (id % per_tile) * (slots.by_head ? 2 : 1)};
-                    }
-                    if (u.len == 0) {
-                        if (lane == 0) id = static_cast<int>(atomicAdd(a.counters, 1u));
-                        continue;
-                    }
+                if (id < group_end) {
+                    unsigned m;
+                    int n;
+                    while (m = __ballot_sync(0xffffffffu, tiles > level), n = __popc(m) * per_tile, id >= level_base + n) level_base += n, --level;
+                    const int rank = (id - level_base) / per_tile;
+                    const int src = __ffs(__ballot_sync(0xffffffffu, ((m >> lane) & 1u) && __popc(m & ((1u << lane) - 1u)) == rank)) - 1;
+                    u = {__shfl_sync(0xffffffffu, first, src), __shfl_sync(0xffffffffu, len, src), level * span,
+                         ((id - level_base) % per_tile) * (slots.by_head ? 2 : 1)};
                 }
                 const bool end_mark = u.len == 0;
-                if (lane == 0 && !end_mark) id = static_cast<int>(atomicAdd(a.counters, 1u));  // known by the time it is needed
+                if (lane == 0 && !end_mark) id = static_cast<int>(gridDim.x + atomicAdd(a.counters, 1u));  // known by the time it is needed
                 const uint32_t us = n_unit % kUnits, ur = n_unit / kUnits;
                 if (ur > 0 && !(ok = wait_warp(bar.unit_empty + us, ur - 1, 51))) break;
                 if (lane == 0) {
@@ -439,18 +447,22 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 float top[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    top[c] = __uint_as_float(x[c][0]);
+                    top[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][31]));
 #pragma unroll
-                    for (int k = 1; k < 31; k += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])));
-                    top[c] = fmaxf(top[c], __uint_as_float(x[c][31]));
+                    for (int k = 1; k < 31; k += 2) top[c] = max3(top[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
                 }
                 const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * f;
-                // the product with the tile before has been done: O may be rescaled, P written
-                if (j > 0) {
-                    if (!(ok = wait_warp(bar.o_done + s, n_s - 1, 61))) break;
-                    tcgen05_fence_after();
-                }
+                // before O is rescaled or P written the product with the tile before has to be done
+                bool may_write = j == 0;
+                auto until_done = [&]() {
+                    if (!may_write) {
+                        may_write = wait_warp(bar.o_done + s, n_s - 1, 61);
+                        tcgen05_fence_after();
+                    }
+                    return may_write;
+                };
                 if (__any_sync(0xffffffffu, best > m + kMaxLead)) {
+                    if (!(ok = until_done())) break;
                     const float now = fmaxf(m, best), mu_new = now == -INFINITY ? 0.f : now;
                     const float shrink = exp2_approx(m - mu_new);  // 0 from -infinity on
                     m = now, mu = mu_new;
@@ -469,23 +481,31 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                 }
                 const float2 ff = make_float2(f, f), sub = make_float2(-mu, -mu);
+                auto quarter = [&](const uint32_t (&w)[32], uint32_t *p) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t p[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        const uint32_t *w = &x[2 * half + k / 16][2 * (k % 16)];
-                        const float2 t = fma2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), ff, sub);
+                    for (int k = 0; k < 16; ++k) {
+                        const float2 t = fma2(make_float2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])), ff, sub);
                         const float2 e = make_float2(exp2_approx(t.x), exp2_approx(t.y));
                         l = add2(l, e);
                         p[k] = E::from_float2(e.x, e.y);
                     }
-                    tcgen05_st_32x32b_x32(tp + 32 * half, p);
+                };
+                auto hand_over = [&](int half) {
                     tcgen05_wait_st();
                     tcgen05_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar.p_half[s] + half);
-                }
+                };
+                uint32_t p0[32], p1[32];
+                quarter(x[0], p0);
+                quarter(x[1], p0 + 16);
+                if (!(ok = until_done())) break;
+                tcgen05_st_32x32b_x32(tp, p0);
+                quarter(x[2], p1);  // while the first half is stored
+                hand_over(0);
+                quarter(x[3], p1 + 16);
+                tcgen05_st_32x32b_x32(tp + 32, p1);
+                hand_over(1);
             }
             if (!ok) break;
             // -------------------------------------------------------- output
@@ -588,7 +608,18 @@ pd_status launch(const PromptArgs &a, cudaStream_t stream) {
     const int64_t ids = tiles * (by_head ? a.q_heads / 2 : a.q_heads);
     if (ids > INT32_MAX / 2) return PD_ERR_UNSUPPORTED_SHAPE;
     const int grid = static_cast<int>(ids < sm_count() ? ids : sm_count());
-    attn_prompt_kernel<D, BF16><<<grid, kThreads, PromptSmem<D>::kTotal, stream>>>(mq, mk, mv, a, static_cast<int>(ids));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = PromptSmem<D>::kTotal;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the set-up may run while the previous kernel drains
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_prompt_kernel<D, BF16>, mq, mk, mv, a);
+    if (e != cudaSuccess) return PD_ERR_CUDA;
     count_launch();
     return cuda_ok(cudaGetLastError());
 }
