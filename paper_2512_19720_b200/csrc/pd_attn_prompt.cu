@@ -57,8 +57,8 @@ struct PromptSmem {
     static constexpr int kStages = D == 128 ? 4 : 8;  // of keys or values
     static constexpr int kQ = 0;
     static constexpr int kRing = 2 * kTileBytes;
-    static constexpr int kOut = kRing + kStages * kTileBytes;  // for each softmax warp 32 rows of 64 outputs
-    static constexpr int kBars = kOut + 8 * 32 * 128;
+    static constexpr int kOut = kRing + kStages * kTileBytes;  // for each softmax warp 32 rows of 32 outputs
+    static constexpr int kBars = kOut + 8 * 32 * 64;
     static constexpr int kTotal = kBars + 1024 + 1024;  // + slack for 1024-byte alignment
     static_assert(kTotal <= 227 * 1024, "shared memory");
 };
@@ -157,6 +157,26 @@ __device__ __forceinline__ uint32_t times_zero(uint32_t w, uint32_t acc) {
     return d;
 }
 
+// Adds to `n` outputs of a row the infinities and NaN among the values of `keys` tokens.
+template <bool BF16>
+__device__ __noinline__ void add_non_finite(uint16_t *y, int n, const uint16_t *v, int64_t token_stride, int keys) {
+    using E = Elem<BF16>;
+    for (int c = 0; c < n; c += 8) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(y + c);
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        for (int key = 0; key < keys; ++key) {
+            const uint4 t = __ldg(reinterpret_cast<const uint4 *>(v + key * token_stride + c));
+            const uint32_t b[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 p = E::to_float2(b[i]), o = E::to_float2(w[i]);
+                w[i] = E::from_float2(fabsf(p.x) <= 3.402823466e38f ? o.x : o.x + p.x, fabsf(p.y) <= 3.402823466e38f ? o.y : o.y + p.y);
+            }
+        }
+        *reinterpret_cast<uint4 *>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -182,7 +202,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         for (int i = 0; i < 4; ++i) mbar_init(bar.v_landed + i, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(bar.q_full + s, 1), mbar_init(bar.q_empty + s, 1), mbar_init(bar.s_full + s, 1);
-            mbar_init(bar.p_half[s], 4), mbar_init(bar.p_half[s] + 1, 4), mbar_init(bar.o_done + s, 1), mbar_init(bar.o_empty + s, 4);
+            mbar_init(bar.p_half[s], 4), mbar_init(bar.p_half[s] + 1, 4), mbar_init(bar.o_done + s, 1);
+            mbar_init(bar.o_empty + s, 4);
         }
         mbar_init(&bar.s_free, 4);
         for (int i = 0; i < kUnits; ++i) mbar_init(bar.unit_full + i, 1), mbar_init(bar.unit_empty + i, 11);
@@ -212,7 +233,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     };
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 8) {
             // -------------------------------------------------------- units and TMA
             // Units in the order of their work, most first, so that the blocks end together: the last queries of every sequence
@@ -402,7 +423,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ------------------------------------------------------------ softmax and output: a thread owns one row of a slot
         const int s = warp >> 2;
         const int r = (warp & 3) * 32 + lane;
@@ -410,16 +431,16 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t ts = lanes + kColS, tp = lanes + kColP + s * 64, to = lanes + kColO + s * 128;
         const float scale2 = a.scale * kLog2e;
         const float f = scale2 > 0.f ? scale2 : (scale2 < 0.f ? -scale2 : 1.f);
-        uint32_t n_s = 0;
+        uint32_t n_s = 0;  // tiles of the slot so far
         bool ok = true;
         Unit u;
         while (ok && next_unit(u)) {
-            const int n = slots.tiles(u, s), row = slots.q0(u, s) + r;
+            const int n = slots.tiles(u, s);
             if (n == 0) {
                 done_unit();
                 continue;
             }
-            float m = -INFINITY, mu = 0.f, l0 = 0.f;
+            float m = -INFINITY, mu = 0.f;
             float2 l = make_float2(0.f, 0.f);
             for (int j = 0; j < n; ++j, ++n_s) {
                 if (!(ok = wait_warp(bar.s_full + s, n_s, 60))) break;
@@ -452,7 +473,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int k = 1; k < 31; k += 2) top[c] = max3(top[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
                 }
                 const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * f;
-                // before O is rescaled or P written the product with the tile before has to be done
+                // Before O is rescaled or P written the product with the tile before has to be done.
                 bool may_write = j == 0;
                 auto until_done = [&]() {
                     if (!may_write) {
@@ -508,57 +529,45 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 hand_over(1);
             }
             if (!ok) break;
-            // -------------------------------------------------------- output
             if (!(ok = wait_warp(bar.o_done + s, n_s - 1, 62))) break;
             tcgen05_fence_after();
-            l0 = l.x + l.y;
-            const float inv = 1.f / l0;
-            const bool taint = bar.taint[n_unit % kUnits] != 0;
-            const int head = slots.head(u, s);
-            const int row0 = slots.q0(u, s) + (warp & 3) * 32;  // the warp's first row
-            uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0) * a.out.token_stride + head * a.out.head_stride;
-            // rows go through shared memory, so that they leave in lines of 128 bytes: written by the threads that own them they
-            // were 32 pieces of 16 bytes an instruction
-            unsigned char *out = smem + L::kOut + warp * (32 * 128);
+            const float inv = 1.f / (l.x + l.y);
+            const int head = slots.head(u, s), row0 = slots.q0(u, s) + (warp & 3) * 32;  // the warp's first row
+            // Rows go through shared memory, so that they leave in pieces of 64 bytes: written by the threads that own them
+            // they were 32 pieces of 16 bytes an instruction.
+            unsigned char *out = smem + L::kOut + warp * (32 * 64);
+            const int piece = lane & 3;
+            uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0 + (lane >> 2)) * a.out.token_stride +
+                          head * a.out.head_stride + 8 * piece;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 64) {
-                uint32_t w[32];
+            for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tcgen05_ld_32x32b_x32(to + c, o);
+                tcgen05_wait_ld();
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t o[32];
-                    tcgen05_ld_32x32b_x32(to + c + 32 * h, o);
-                    tcgen05_wait_ld();
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t x[4];
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * inv);
-                    if (taint && row < u.len) {
-                        const uint16_t *v = static_cast<const uint16_t *>(a.v.ptr) + (head / group) * a.v.head_stride + c + 32 * h;
-                        for (int key = u.q0; key <= row; ++key)
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) {
-                                const float t = E::to_float(v[static_cast<int64_t>(u.first + key) * a.v.token_stride + k]);
-                                if (!(fabsf(t) <= 3.402823466e38f)) o[k] = __float_as_uint(__uint_as_float(o[k]) + t);
-                            }
-                    }
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) w[16 * h + k] = E::from_float2(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+                    for (int i = 0; i < 4; ++i) x[i] = E::from_float2(__uint_as_float(o[8 * k + 2 * i]) * inv, __uint_as_float(o[8 * k + 2 * i + 1]) * inv);
+                    *reinterpret_cast<uint4 *>(out + lane * 64 + ((k ^ ((lane >> 1) & 3)) * 16)) = make_uint4(x[0], x[1], x[2], x[3]);
                 }
-                if (c + 64 == D) {  // O has been read
-                    tcgen05_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar.o_empty + s);
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    *reinterpret_cast<uint4 *>(out + lane * 128 + ((k ^ (lane & 7)) * 16)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+                if (c + 32 == D) tcgen05_fence_before();
                 __syncwarp();
+                if (c + 32 == D && lane == 0) mbar_arrive(bar.o_empty + s);  // O has been read
+                uint16_t *row = y + c;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int i = 4 * k + (lane >> 3), piece = lane & 7;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(out + i * 128 + ((piece ^ (i & 7)) * 16));
-                    if (row0 + i < u.len) *reinterpret_cast<uint4 *>(y + i * a.out.token_stride + c + 8 * piece) = x;
+                for (int k = 0; k < 4; ++k, row += 8 * a.out.token_stride) {
+                    const int i = 8 * k + (lane >> 2);
+                    const uint4 x = *reinterpret_cast<const uint4 *>(out + i * 64 + ((piece ^ ((i >> 1) & 3)) * 16));
+                    if (row0 + i < u.len) *reinterpret_cast<uint4 *>(row) = x;
                 }
                 __syncwarp();
             }
+            if (bar.taint[n_unit % kUnits] && row0 + lane < u.len)
+                add_non_finite<BF16>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0 + lane) * a.out.token_stride +
+                                         head * a.out.head_stride, D,
+                                     static_cast<const uint16_t *>(a.v.ptr) + static_cast<int64_t>(u.first + u.q0) * a.v.token_stride +
+                                         (head / group) * a.v.head_stride, a.v.token_stride, row0 + lane - u.q0 + 1);
             done_unit();
         }
     }
