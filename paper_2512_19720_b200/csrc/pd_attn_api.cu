@@ -92,9 +92,10 @@ pd_status cache_impl(HeadsView q, int32_t n_seqs, int32_t q_heads, int32_t kv_he
                      size_t workspace_bytes, void *cuda_stream, bool bf16) {
     if (n_seqs <= 0) return PD_ERR_INVALID_ARG;
     PD_TRY(check_heads(q_heads, kv_heads, head_dim, scale));
-    // the tiles of all sequences are counted in 32 bits
-    if (static_cast<int64_t>(n_seqs) * table_width > INT_MAX / 4 || n_seqs > INT_MAX / 4) return PD_ERR_UNSUPPORTED_SHAPE;
     PD_TRY(check_cache(k_codes, v_codes, k_scale, v_scale, n_pages, page, seq_lens, block_table, table_stride, table_width));
+    // tiles of at least 16 tokens are counted in 32 bits, for all sequences and heads together
+    const int64_t tiles = static_cast<int64_t>(table_width) * (page / 16) + 1;
+    if (tiles > INT_MAX / 2 || tiles * n_seqs > INT_MAX / 2 || tiles * n_seqs * q_heads > INT_MAX / 2) return PD_ERR_UNSUPPORTED_SHAPE;
     PD_TRY(check_view(q, n_seqs, q_heads, head_dim));
     PD_TRY(check_view(out, n_seqs, q_heads, head_dim));
     PD_TRY(check_workspace(workspace, workspace_bytes));

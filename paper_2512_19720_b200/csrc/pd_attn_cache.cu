@@ -27,8 +27,9 @@ namespace pd {
 namespace {
 
 constexpr int kTile = 32;    // tokens of a tile: a multiple of 16, so that a 16-token product lies in one page
-constexpr int kMaxGrid = 1024;  // counters in the workspace
-constexpr size_t kCounterBytes = kMaxGrid * 4;
+constexpr int kMaxGrid = 1024;
+constexpr int kMaxRows = 16;    // heads of a segment
+constexpr size_t kCounterBytes = kMaxGrid * kMaxRows * 4;  // for each block and row: parts of the segment that goes on behind the block
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLead = 8.f;         // how far (base-2 exponent) a score may pass the reference maximum
 
@@ -47,7 +48,7 @@ struct CacheShape {
     // being used), the last one takes the ring's.
     static constexpr int kTotal = kWarps * (kWarp + kPiece);
     static_assert(kPiece <= kRing && kWarp % 16 == 0 && kPiece % 16 == 0, "layout");
-    static_assert(kTotal <= 225 * 1024, "shared memory");
+    static_assert(2 * kThreads * 4 <= kWarps * kPiece && kTotal <= 226 * 1024, "shared memory");
 };
 
 __device__ __forceinline__ float exp2_approx(float x) {
@@ -76,7 +77,7 @@ __device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + kTile
 
 // A partial result of a segment in a warp's shared memory: which one, and where it starts in the order of all tiles.
 struct Piece {
-    int64_t first;  // the segment's first tile; -1: none
+    int first;  // the segment's first tile; -1: none
     int tiles, b, head0, rows;
 };
 
@@ -90,10 +91,11 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     constexpr int KC = D / 64;      // 16-byte pieces of a key that a thread takes
     constexpr int VB = D / 8;       // bytes of a value that a thread takes
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int scan[kThreads];
+    static_assert(L::kRows <= kMaxRows && kThreads % 32 == 0, "layout");
+    // until every warp has found its first tile: where the first partial results go later
+    int *scan = reinterpret_cast<int *>(smem + kWarps * L::kWarp), *scan_len = scan + kThreads;
     __shared__ int warp_sum[kWarps];
     __shared__ Piece pieces[kWarps][2];
-    __shared__ unsigned int arrived;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
@@ -108,13 +110,16 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         return n < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(n), room));
     };
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while the previous kernel drains
     // ---------------------------------------------------------------- tiles before each thread's share of the sequences
     const int share = (a.n_seqs + kThreads - 1) / kThreads;
-    int sum = 0;
+    int sum = 0, first_len = 0;
     for (int b = threadIdx.x * share; b < min(a.n_seqs, static_cast<int>(threadIdx.x + 1) * share); ++b) {
-        const int n = __ldg(a.seq_lens + b);
-        if (blockIdx.x == 0 && (n < 0 || n > room)) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
-        sum += tiles_of(length(b));
+        const int raw = __ldg(a.seq_lens + b), n = length(b);
+        if (blockIdx.x == 0 && raw != n) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
+        if (b == static_cast<int>(threadIdx.x) * share) first_len = n;
+        sum += tiles_of(n);
     }
     int incl = sum;
 #pragma unroll
@@ -131,32 +136,34 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         total_seq += warp_sum[w];
     }
     scan[threadIdx.x] = before + incl - sum;
+    scan_len[threadIdx.x] = first_len;
     __syncthreads();
-    const int64_t total = static_cast<int64_t>(total_seq) * per_seq;
+    const int total = total_seq * per_seq;  // the host has seen to it that 32 bits are enough
     // At least a tile for each warp of a block: with fewer, a segment would be joined from more parts than it has tiles.
-    const int n_ctas = static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), total / kWarps)));
+    const int n_ctas = max(1, min(static_cast<int>(gridDim.x), total / kWarps));
     if (static_cast<int>(blockIdx.x) >= n_ctas) return;
-    auto cta_first = [&](int64_t c) { return total * c / n_ctas; };  // first tile of a block's range
-    const int64_t cta0 = cta_first(blockIdx.x), cta1 = cta_first(blockIdx.x + 1);
-    const int64_t range0 = cta0 + (cta1 - cta0) * warp / kWarps, range1 = cta0 + (cta1 - cta0) * (warp + 1) / kWarps;
+    const int quota = total / n_ctas, more = total - quota * n_ctas;  // the first `more` blocks take a tile more
+    auto cta_first = [&](int c) { return c * quota + min(c, more); };
+    auto cta_of = [&](int tile) { return tile < more * (quota + 1) ? tile / (quota + 1) : more + (tile - more * (quota + 1)) / quota; };
+    const int cta0 = cta_first(blockIdx.x), cta1 = cta_first(blockIdx.x + 1);
+    const int warp_quota = (cta1 - cta0) / kWarps, warp_more = (cta1 - cta0) % kWarps;
+    const int range0 = cta0 + warp * warp_quota + min(warp, warp_more), range1 = range0 + warp_quota + (warp < warp_more ? 1 : 0);
 
     // Finds the segment of a tile: sequence b, segment s of it, tile i of the segment.
-    auto locate = [&](int64_t at, int &b, int &s, int &i, int &len) {
-        int lo = 0, hi = kThreads - 1;  // the last share that starts at or before the tile
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (static_cast<int64_t>(scan[mid]) * per_seq <= at) lo = mid;
-            else hi = mid - 1;
-        }
+    auto locate = [&](int at, int &b, int &s, int &i, int &len) {
+        const int seq_tile = at / per_seq;  // a share starts at or before the tile where it starts at or before this
+        constexpr int kStep = kThreads / 32;
+        int lo = (31 - __clz(__ballot_sync(0xffffffffu, scan[lane * kStep] <= seq_tile))) * kStep;
+        lo += 31 - __clz(__ballot_sync(0xffffffffu, lane < kStep && scan[lo + min(lane, kStep - 1)] <= seq_tile));
         b = lo * share;
-        int64_t rest = at - static_cast<int64_t>(scan[lo]) * per_seq;
-        len = length(b);
-        while (rest >= static_cast<int64_t>(tiles_of(len)) * per_seq && b + 1 < a.n_seqs) {
-            rest -= static_cast<int64_t>(tiles_of(len)) * per_seq;
+        len = scan_len[lo];
+        int rest = at - scan[lo] * per_seq;
+        while (rest >= tiles_of(len) * per_seq && b + 1 < a.n_seqs) {
+            rest -= tiles_of(len) * per_seq;
             len = length(++b);
         }
-        s = static_cast<int>(rest / tiles_of(len));
-        i = static_cast<int>(rest - static_cast<int64_t>(s) * tiles_of(len));
+        s = rest / tiles_of(len);
+        i = rest - s * tiles_of(len);
     };
 
     unsigned char *ring = smem + warp * L::kWarp;
@@ -166,14 +173,15 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     // ---------------------------------------------------------------- the warp's tiles
     const float lscale = a.scale * kLog2e;
     int b = 0, s = 0, i0 = 0, len = 0;
-    int64_t at = range0;
+    int at = range0;
     if (at < range1) locate(at, b, s, i0, len);
+    __syncthreads();
     while (at < range1) {
         const int n_tiles = tiles_of(len);
         const int kvh = s / chunks, chunk = s - kvh * chunks;
         const int head0 = kvh * group + chunk * L::kRows;
         const int rows = min(L::kRows, group - chunk * L::kRows);
-        const int i1 = static_cast<int>(min(static_cast<int64_t>(n_tiles), i0 + (range1 - at)));
+        const int i1 = min(n_tiles, i0 + (range1 - at));
 
         float o[MT][NT][4];
         float m[NT][2], mu[NT][2], l[NT][2], qs[NT][2];
@@ -257,7 +265,6 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                     }
                     const int st = (i - i0) % kStages;
                     const int src = i - base;
-                    if (lane == src) meta[st] = make_float4(sk[0], sk[1], sv[0], sv[1]);
                     unsigned char *kdst = ring + st * L::kStage, *vdst = kdst + kTile * D;
                     constexpr int kPieces = D / 16, kRowsPer = 32 / kPieces;
                     const int c = lane % kPieces;
@@ -277,6 +284,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                             }
                         }
                     }
+                    if (lane == src) meta[st] = make_float4(sk[0], sk[1], sv[0], sv[1]);  // after the copies: the scales may still be on their way
                 }
                 cp_async_commit();
             };
@@ -449,14 +457,32 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     __syncthreads();
 
     // ---------------------------------------------------------------- the block's parts of each segment, in the order of the tiles
-    auto store_out = [&](const Piece &p, int r, int d, float4 v, float f) {
-        uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + p.b * a.out.token_stride + (p.head0 + r) * a.out.head_stride + d;
-        *reinterpret_cast<uint2 *>(y) = make_uint2(E::from_float2(v.x * f, v.y * f), E::from_float2(v.z * f, v.w * f));
+    // A warp takes a row at a time, a lane D / 32 of its outputs.  Rows of a segment that other blocks hold parts of are joined
+    // by the last block that has written its own.
+    constexpr int kPartial = L::kPiece / 4;
+    constexpr int V = D / 32;
+    struct Sum {
+        float top, l, o[V];
     };
     auto weight = [](float m, float top) { return m == -INFINITY ? 0.f : exp2_approx(m - top); };
-    constexpr int kPartial = L::kPiece / 4;
-    Piece open[2];  // segments that other blocks hold parts of: the one that started before this block's range, the one that goes on behind it
-    open[0].first = open[1].first = -1;
+    auto load_o = [](const float *p, float (&o)[V], bool global) {
+        if (V == 4) {
+            const float4 x = global ? __ldcg(reinterpret_cast<const float4 *>(p)) : *reinterpret_cast<const float4 *>(p);
+            o[0] = x.x, o[1] = x.y, o[V - 2] = x.z, o[V - 1] = x.w;
+        } else {
+            const float2 x = global ? __ldcg(reinterpret_cast<const float2 *>(p)) : *reinterpret_cast<const float2 *>(p);
+            o[0] = x.x, o[1] = x.y;
+        }
+    };
+    auto store_out = [&](const Piece &p, int r, const Sum &x) {
+        const float f = x.l == 0.f ? 0.f : 1.f / x.l;
+        uint32_t *y = reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + p.b * a.out.token_stride +
+                                                   (p.head0 + r) * a.out.head_stride + V * lane);
+        if (V == 4) *reinterpret_cast<uint2 *>(y) = make_uint2(E::from_float2(x.o[0] * f, x.o[1] * f), E::from_float2(x.o[V - 2] * f, x.o[V - 1] * f));
+        else *y = E::from_float2(x.o[0] * f, x.o[1] * f);
+    };
+    auto part_of = [&](int cta, int slot) { return a.partial + (static_cast<size_t>(cta) * 2 + slot) * kPartial; };
+    int item = 0;  // rows of the segments so far
     for (int w0 = 0; w0 < 2 * kWarps;) {
         const Piece p = pieces[w0 >> 1][w0 & 1];
         int w1 = w0 + 1;
@@ -466,76 +492,68 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         }
         while (w1 < 2 * kWarps && (pieces[w1 >> 1][w1 & 1].first < 0 || pieces[w1 >> 1][w1 & 1].first == p.first)) ++w1;
         const bool mine = p.first >= cta0 && p.first + p.tiles <= cta1;
-        const int slot = p.first < cta0 ? 0 : 1;
-        float *out_part = a.partial + (static_cast<size_t>(blockIdx.x) * 2 + slot) * kPartial;
-        for (int idx = threadIdx.x; idx < p.rows * (D / 4); idx += kThreads) {
-            const int r = idx / (D / 4), d = idx % (D / 4) * 4;
-            float top = -INFINITY;
+        for (int r = (warp + kWarps - item % kWarps) % kWarps; r < p.rows; r += kWarps) {
+            Sum x = {-INFINITY, 0.f, {}};
             for (int w = w0; w < w1; ++w)
-                if (pieces[w >> 1][w & 1].first >= 0) top = fmaxf(top, piece_at(w >> 1, w & 1)[L::kRows * D + r]);
-            float4 sum4 = make_float4(0.f, 0.f, 0.f, 0.f);
-            float sum_l = 0.f;
+                if (pieces[w >> 1][w & 1].first >= 0) x.top = fmaxf(x.top, piece_at(w >> 1, w & 1)[L::kRows * D + r]);
             for (int w = w0; w < w1; ++w) {
                 if (pieces[w >> 1][w & 1].first < 0) continue;
                 const float *po = piece_at(w >> 1, w & 1);
-                const float f = weight(po[L::kRows * D + r], top);
-                const float4 v = *reinterpret_cast<const float4 *>(po + r * D + d);
-                sum4.x = fmaf(v.x, f, sum4.x), sum4.y = fmaf(v.y, f, sum4.y), sum4.z = fmaf(v.z, f, sum4.z), sum4.w = fmaf(v.w, f, sum4.w);
-                sum_l = fmaf(po[L::kRows * D + L::kRows + r], f, sum_l);
+                const float f = weight(po[L::kRows * D + r], x.top);
+                float o[V];
+                load_o(po + r * D + V * lane, o, false);
+#pragma unroll
+                for (int k = 0; k < V; ++k) x.o[k] = fmaf(o[k], f, x.o[k]);
+                x.l = fmaf(po[L::kRows * D + L::kRows + r], f, x.l);
             }
             if (mine) {
-                store_out(p, r, d, sum4, sum_l == 0.f ? 0.f : 1.f / sum_l);
-            } else {
-                *reinterpret_cast<float4 *>(out_part + r * D + d) = sum4;
-                if (d == 0) out_part[L::kRows * D + r] = top, out_part[L::kRows * D + L::kRows + r] = sum_l;
+                store_out(p, r, x);
+                continue;
             }
-        }
-        if (!mine) open[slot] = p;
-        w0 = w1;
-    }
-
-    // ---------------------------------------------------------------- segments that several blocks worked on: the last block to arrive joins them
-    for (int slot = 0; slot < 2; ++slot) {
-        const Piece p = open[slot];
-        if (p.first < 0) continue;  // the same in all threads
-        const int c0 = static_cast<int>(((p.first + 1) * n_ctas - 1) / total), c1 = static_cast<int>(((p.first + p.tiles) * n_ctas - 1) / total);
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) arrived = atomicAdd(a.counters + c0, 1u);
-        __syncthreads();
-        if (arrived != static_cast<unsigned int>(c1 - c0)) continue;
-        __threadfence();
-        if (threadIdx.x == 0) a.counters[c0] = 0u;
-        for (int idx = threadIdx.x; idx < p.rows * (D / 4); idx += kThreads) {
-            const int r = idx / (D / 4), d = idx % (D / 4) * 4;
-            float4 sum4 = make_float4(0.f, 0.f, 0.f, 0.f);
-            float sum_l = 0.f, top = -INFINITY;
-            for (int c = c0; c <= c1; c += 4) {
-                float pm[4], pl[4];
-                float4 pv[4];
+            float *mine_part = part_of(blockIdx.x, p.first < cta0 ? 0 : 1);
+            if (V == 4) *reinterpret_cast<float4 *>(mine_part + r * D + V * lane) = make_float4(x.o[0], x.o[1], x.o[V - 2], x.o[V - 1]);
+            else *reinterpret_cast<float2 *>(mine_part + r * D + V * lane) = make_float2(x.o[0], x.o[1]);
+            if (lane == 0) mine_part[L::kRows * D + r] = x.top, mine_part[L::kRows * D + L::kRows + r] = x.l;
+            __threadfence();
+            __syncwarp();
+            const int c0 = cta_of(p.first), c1 = cta_of(p.first + p.tiles - 1);
+            unsigned int arrived = 0;
+            if (lane == 0) arrived = atomicAdd(a.counters + c0 * kMaxRows + r, 1u);
+            if (__shfl_sync(0xffffffffu, arrived, 0) != static_cast<unsigned int>(c1 - c0)) continue;
+            __threadfence();
+            if (lane == 0) a.counters[c0 * kMaxRows + r] = 0u;
+            x = {-INFINITY, 0.f, {}};
+            constexpr int kBatch = 8;
+            for (int c = c0; c <= c1; c += kBatch) {
+                float pm[kBatch], pl[kBatch], po[kBatch][V], now = x.top;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < kBatch; ++k) {
                     const int cc = min(c + k, c1);
-                    // only the segment's first block may hold it as its last one
-                    const float *po = a.partial + (static_cast<size_t>(cc) * 2 + (p.first < cta_first(cc) ? 0 : 1)) * kPartial;
-                    pm[k] = c + k <= c1 ? __ldcg(po + L::kRows * D + r) : -INFINITY;
-                    pl[k] = __ldcg(po + L::kRows * D + L::kRows + r);
-                    pv[k] = __ldcg(reinterpret_cast<const float4 *>(po + r * D + d));
+                    const float *part = part_of(cc, p.first < cta_first(cc) ? 0 : 1);  // only the first block has it as its last segment
+                    pm[k] = c + k <= c1 ? __ldcg(part + L::kRows * D + r) : -INFINITY;
+                    pl[k] = __ldcg(part + L::kRows * D + L::kRows + r);
+                    load_o(part + r * D + V * lane, po[k], true);
                 }
-                const float now = fmaxf(top, fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])));
-                const float f0 = weight(top, now);
-                sum4.x *= f0, sum4.y *= f0, sum4.z *= f0, sum4.w *= f0, sum_l *= f0;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < kBatch; ++k) now = fmaxf(now, pm[k]);
+                const float f0 = weight(x.top, now);
+                x.l *= f0;
+#pragma unroll
+                for (int i = 0; i < V; ++i) x.o[i] *= f0;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
                     if (c + k > c1) break;
                     const float f = weight(pm[k], now);
-                    sum4.x = fmaf(pv[k].x, f, sum4.x), sum4.y = fmaf(pv[k].y, f, sum4.y), sum4.z = fmaf(pv[k].z, f, sum4.z), sum4.w = fmaf(pv[k].w, f, sum4.w);
-                    sum_l = fmaf(pl[k], f, sum_l);
+                    x.l = fmaf(pl[k], f, x.l);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) x.o[i] = fmaf(po[k][i], f, x.o[i]);
                 }
-                top = now;
+                x.top = now;
             }
-            store_out(p, r, d, sum4, sum_l == 0.f ? 0.f : 1.f / sum_l);
+            store_out(p, r, x);
         }
+        item += p.rows;
+        w0 = w1;
     }
 }
 
@@ -544,9 +562,18 @@ pd_status launch(const CacheAttnArgs &a, int grid, cudaStream_t stream) {
     using L = CacheShape<D, NT>;
     static std::atomic<bool> done[kMaxDevices];
     if (!ensure_dynamic_smem(attn_cache_kernel<D, NT, BF16>, L::kTotal, done)) return PD_ERR_CUDA;
-    attn_cache_kernel<D, NT, BF16><<<grid, L::kThreads, L::kTotal, stream>>>(a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.blockDim = dim3(L::kThreads);
+    cfg.dynamicSmemBytes = L::kTotal;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     count_launch();
-    return cuda_ok(cudaGetLastError());
+    return cuda_ok(cudaLaunchKernelEx(&cfg, attn_cache_kernel<D, NT, BF16>, a));
 }
 
 }  // namespace

@@ -39,7 +39,9 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
     // Sequence b's pages are the ids from cu[b] / page + 2 b on: there are never more of them than ids before the next
     // sequence's, so that the page of a block is found from the offsets alone.
     if (threadIdx.x == 0) found = 0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while the previous kernel drains
     int mine = 0;
     for (int b = threadIdx.x; b < a.n_seqs; b += blockDim.x)
         if ((min(max(__ldg(a.cu_seqlens + b), 0), a.n_tokens) >> a.page_log2) + 2 * b <= id) mine = b;  // ascending in b
@@ -147,9 +149,17 @@ pd_status launch_kv_append(const AppendArgs &a, bool bf16, cudaStream_t stream) 
     const int threads = max(32, min(256, page * a.head_dim / (8 * kVecs)));
     auto kernel = a.head_dim == 128 ? (bf16 ? kv_append_kernel<128, true> : kv_append_kernel<128, false>)
                                     : (bf16 ? kv_append_kernel<64, true> : kv_append_kernel<64, false>);
-    kernel<<<grid, threads, 0, stream>>>(a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     count_launch();
-    return cuda_ok(cudaGetLastError());
+    return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, a));
 }
 
 }  // namespace pd
