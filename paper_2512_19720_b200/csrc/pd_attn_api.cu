@@ -33,7 +33,7 @@ pd_status check_cache(const void *k_codes, const void *v_codes, const float *k_s
                       const int32_t *seq_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width) {
     if (!k_codes || !v_codes || !k_scale || !v_scale || n_pages <= 0 || !seq_lens || !block_table || table_width <= 0 || table_stride < table_width)
         return PD_ERR_INVALID_ARG;
-    if (page != 16 && page != 32 && page != 64 && page != 128) return PD_ERR_UNSUPPORTED_SHAPE;
+    if ((page != 16 && page != 32 && page != 64 && page != 128) || static_cast<int64_t>(table_width) * page > INT_MAX / 2) return PD_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(k_codes) || !aligned16(v_codes)) return PD_ERR_ALIGNMENT;
     if ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale) | reinterpret_cast<uintptr_t>(seq_lens) |
          reinterpret_cast<uintptr_t>(block_table)) & 3u)

@@ -183,6 +183,65 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         const int rows = min(L::kRows, group - chunk * L::kRows);
         const int i1 = min(n_tiles, i0 + (range1 - at));
 
+        // lane j holds page and scales of tile base + j (two pages where a page is half a tile)
+        int base = i0 - 32;
+        int64_t pid[2] = {0, 0};
+        float sk[2] = {0.f, 0.f}, sv[2] = {0.f, 0.f};
+        auto issue = [&](int i) {
+            if (i < i1) {
+                if (i - base >= 32) {
+                    base = i;
+                    const int mine = i + lane;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int64_t tok = static_cast<int64_t>(mine) * kTile + 16 * k;
+                        pid[k] = 0, sk[k] = 0.f, sv[k] = 0.f;
+                        if (mine < i1 && tok < len) {
+                            if (k == 1 && page > 16) {
+                                pid[k] = pid[0], sk[k] = sk[0], sv[k] = sv[0];
+                            } else {
+                                const int64_t p = __ldg(a.block_table + b * a.table_stride + (tok >> a.page_log2));
+                                if (p < 0 || p >= a.n_pages) {
+                                    latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
+                                } else {
+                                    pid[k] = p;
+                                    sk[k] = a.pages[0].scale[p * a.kv_heads + kvh];
+                                    sv[k] = a.pages[1].scale[p * a.kv_heads + kvh];
+                                }
+                            }
+                        }
+                    }
+                }
+                const int st = (i - i0) % kStages;
+                const int src = i - base;
+                unsigned char *kdst = ring + st * L::kStage, *vdst = kdst + kTile * D;
+                constexpr int kPieces = D / 16, kRowsPer = 32 / kPieces;
+                const int c = lane % kPieces;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int64_t p = __shfl_sync(0xffffffffu, pid[half], src);
+                    const int64_t tok = static_cast<int64_t>(i) * kTile + 16 * half;
+                    const int64_t off = (((p * a.kv_heads + kvh) << a.page_log2) + (tok & (page - 1))) * D;
+#pragma unroll
+                    for (int k = 0; k < 16 / kRowsPer; ++k) {
+                        const int r = k * kRowsPer + lane / kPieces, row = 16 * half + r;
+                        if (tok + r < len) {
+                            const int ck = D == 128 ? c ^ ((row & 1) * 4) : c;
+                            const int cv = D == 128 ? c ^ (row & 6) : c;
+                            cp_async16(kdst + row * D + ck * 16, a.pages[0].codes + off + r * D + c * 16);
+                            cp_async16(vdst + row * D + cv * 16, a.pages[1].codes + off + r * D + c * 16);
+                        }
+                    }
+                }
+                if (lane == src) meta[st] = make_float4(sk[0], sk[1], sv[0], sv[1]);  // after the copies: the scales may still be on their way
+            }
+            cp_async_commit();
+        };
+        __syncwarp();
+        if (len > 0) {
+#pragma unroll
+            for (int k = 0; k < kStages - 1; ++k) issue(i0 + k);
+        }
         float o[MT][NT][4];
         float m[NT][2], mu[NT][2], l[NT][2], qs[NT][2];
         uint32_t qf[KS][NT][2];
@@ -234,63 +293,6 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         }
 
         if (len > 0) {
-            // lane j holds page and scales of tile base + j (two pages where a page is half a tile)
-            int base = i0 - 32;
-            int64_t pid[2] = {0, 0};
-            float sk[2] = {0.f, 0.f}, sv[2] = {0.f, 0.f};
-            auto issue = [&](int i) {
-                if (i < i1) {
-                    if (i - base >= 32) {
-                        base = i;
-                        const int mine = i + lane;
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const int64_t tok = static_cast<int64_t>(mine) * kTile + 16 * k;
-                            pid[k] = 0, sk[k] = 0.f, sv[k] = 0.f;
-                            if (mine < i1 && tok < len) {
-                                if (k == 1 && page > 16) {
-                                    pid[k] = pid[0], sk[k] = sk[0], sv[k] = sv[0];
-                                } else {
-                                    const int64_t p = __ldg(a.block_table + b * a.table_stride + (tok >> a.page_log2));
-                                    if (p < 0 || p >= a.n_pages) {
-                                        latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
-                                    } else {
-                                        pid[k] = p;
-                                        sk[k] = a.pages[0].scale[p * a.kv_heads + kvh];
-                                        sv[k] = a.pages[1].scale[p * a.kv_heads + kvh];
-                                    }
-                                }
-                            }
-                        }
-                    }
-                    const int st = (i - i0) % kStages;
-                    const int src = i - base;
-                    unsigned char *kdst = ring + st * L::kStage, *vdst = kdst + kTile * D;
-                    constexpr int kPieces = D / 16, kRowsPer = 32 / kPieces;
-                    const int c = lane % kPieces;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const int64_t p = __shfl_sync(0xffffffffu, pid[half], src);
-                        const int64_t tok = static_cast<int64_t>(i) * kTile + 16 * half;
-                        const int64_t off = (((p * a.kv_heads + kvh) << a.page_log2) + (tok & (page - 1))) * D;
-#pragma unroll
-                        for (int k = 0; k < 16 / kRowsPer; ++k) {
-                            const int r = k * kRowsPer + lane / kPieces, row = 16 * half + r;
-                            if (tok + r < len) {
-                                const int ck = D == 128 ? c ^ ((row & 1) * 4) : c;
-                                const int cv = D == 128 ? c ^ (row & 6) : c;
-                                cp_async16(kdst + row * D + ck * 16, a.pages[0].codes + off + r * D + c * 16);
-                                cp_async16(vdst + row * D + cv * 16, a.pages[1].codes + off + r * D + c * 16);
-                            }
-                        }
-                    }
-                    if (lane == src) meta[st] = make_float4(sk[0], sk[1], sv[0], sv[1]);  // after the copies: the scales may still be on their way
-                }
-                cp_async_commit();
-            };
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < kStages - 1; ++k) issue(i0 + k);
             for (int i = i0; i < i1; ++i) {
                 cp_async_wait<kStages - 2>();
                 __syncwarp();
@@ -482,22 +484,30 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         else *y = E::from_float2(x.o[0] * f, x.o[1] * f);
     };
     auto part_of = [&](int cta, int slot) { return a.partial + (static_cast<size_t>(cta) * 2 + slot) * kPartial; };
-    int item = 0;  // rows of the segments so far
-    for (int w0 = 0; w0 < 2 * kWarps;) {
+    // where each segment's parts begin among the warps' pieces: entry 2 w + slot
+    const int my_first = lane < 2 * kWarps ? pieces[lane >> 1][lane & 1].first : -1;
+    const unsigned valid = __ballot_sync(0xffffffffu, my_first >= 0);
+    const unsigned below = valid & ((1u << lane) - 1u);
+    const int first_before = __shfl_sync(0xffffffffu, my_first, below ? 31 - __clz(below) : lane);
+    unsigned heads = __ballot_sync(0xffffffffu, my_first >= 0 && (!below || first_before != my_first));
+    int open[2] = {-1, -1}, open_item[2] = {0, 0};  // entries of the segments that other blocks hold parts of: started before this one, goes on behind it
+    int item = 0;                                   // rows of the segments so far; row r of a segment falls to warp (item + r) % kWarps
+    while (heads) {
+        const int w0 = __ffs(heads) - 1;
+        heads &= heads - 1;
+        const unsigned own = valid & (heads ? (1u << (__ffs(heads) - 1)) - 1u : 0xffffffffu) & ~((1u << w0) - 1u);
         const Piece p = pieces[w0 >> 1][w0 & 1];
-        int w1 = w0 + 1;
-        if (p.first < 0) {
-            w0 = w1;
-            continue;
-        }
-        while (w1 < 2 * kWarps && (pieces[w1 >> 1][w1 & 1].first < 0 || pieces[w1 >> 1][w1 & 1].first == p.first)) ++w1;
         const bool mine = p.first >= cta0 && p.first + p.tiles <= cta1;
+        const int slot = p.first < cta0 ? 0 : 1;
+        if (!mine) open[slot] = w0, open_item[slot] = item;
         for (int r = (warp + kWarps - item % kWarps) % kWarps; r < p.rows; r += kWarps) {
             Sum x = {-INFINITY, 0.f, {}};
-            for (int w = w0; w < w1; ++w)
-                if (pieces[w >> 1][w & 1].first >= 0) x.top = fmaxf(x.top, piece_at(w >> 1, w & 1)[L::kRows * D + r]);
-            for (int w = w0; w < w1; ++w) {
-                if (pieces[w >> 1][w & 1].first < 0) continue;
+            for (unsigned m = own; m; m &= m - 1) {
+                const int w = __ffs(m) - 1;
+                x.top = fmaxf(x.top, piece_at(w >> 1, w & 1)[L::kRows * D + r]);
+            }
+            for (unsigned m = own; m; m &= m - 1) {
+                const int w = __ffs(m) - 1;
                 const float *po = piece_at(w >> 1, w & 1);
                 const float f = weight(po[L::kRows * D + r], x.top);
                 float o[V];
@@ -510,50 +520,64 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                 store_out(p, r, x);
                 continue;
             }
-            float *mine_part = part_of(blockIdx.x, p.first < cta0 ? 0 : 1);
-            if (V == 4) *reinterpret_cast<float4 *>(mine_part + r * D + V * lane) = make_float4(x.o[0], x.o[1], x.o[V - 2], x.o[V - 1]);
-            else *reinterpret_cast<float2 *>(mine_part + r * D + V * lane) = make_float2(x.o[0], x.o[1]);
-            if (lane == 0) mine_part[L::kRows * D + r] = x.top, mine_part[L::kRows * D + L::kRows + r] = x.l;
-            __threadfence();
-            __syncwarp();
-            const int c0 = cta_of(p.first), c1 = cta_of(p.first + p.tiles - 1);
-            unsigned int arrived = 0;
-            if (lane == 0) arrived = atomicAdd(a.counters + c0 * kMaxRows + r, 1u);
-            if (__shfl_sync(0xffffffffu, arrived, 0) != static_cast<unsigned int>(c1 - c0)) continue;
-            __threadfence();
-            if (lane == 0) a.counters[c0 * kMaxRows + r] = 0u;
-            x = {-INFINITY, 0.f, {}};
-            constexpr int kBatch = 8;
-            for (int c = c0; c <= c1; c += kBatch) {
-                float pm[kBatch], pl[kBatch], po[kBatch][V], now = x.top;
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    const int cc = min(c + k, c1);
-                    const float *part = part_of(cc, p.first < cta_first(cc) ? 0 : 1);  // only the first block has it as its last segment
-                    pm[k] = c + k <= c1 ? __ldcg(part + L::kRows * D + r) : -INFINITY;
-                    pl[k] = __ldcg(part + L::kRows * D + L::kRows + r);
-                    load_o(part + r * D + V * lane, po[k], true);
-                }
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k) now = fmaxf(now, pm[k]);
-                const float f0 = weight(x.top, now);
-                x.l *= f0;
-#pragma unroll
-                for (int i = 0; i < V; ++i) x.o[i] *= f0;
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    if (c + k > c1) break;
-                    const float f = weight(pm[k], now);
-                    x.l = fmaf(pl[k], f, x.l);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) x.o[i] = fmaf(po[k][i], f, x.o[i]);
-                }
-                x.top = now;
-            }
-            store_out(p, r, x);
+            float *part = part_of(blockIdx.x, slot);
+            if (V == 4) *reinterpret_cast<float4 *>(part + r * D + V * lane) = make_float4(x.o[0], x.o[1], x.o[V - 2], x.o[V - 1]);
+            else *reinterpret_cast<float2 *>(part + r * D + V * lane) = make_float2(x.o[0], x.o[1]);
+            if (lane == 0) part[L::kRows * D + r] = x.top, part[L::kRows * D + L::kRows + r] = x.l;
         }
         item += p.rows;
-        w0 = w1;
+    }
+    if (open[0] < 0 && open[1] < 0) return;
+    // One fence for all rows that the warp has written, then a lane for each row of the two open segments.
+    __threadfence();
+    __syncwarp();
+    const int my_slot = lane >> 4, my_row = lane & 15;
+    bool last = false;
+    if (open[my_slot] >= 0) {
+        const Piece p = pieces[open[my_slot] >> 1][open[my_slot] & 1];
+        if (my_row < p.rows && (open_item[my_slot] + my_row) % kWarps == warp) {
+            const int c0 = cta_of(p.first), c1 = cta_of(p.first + p.tiles - 1);
+            unsigned int *counter = a.counters + c0 * kMaxRows + my_row;
+            last = atomicAdd(counter, 1u) == static_cast<unsigned int>(c1 - c0);
+            if (last) *counter = 0u;
+        }
+    }
+    unsigned todo = __ballot_sync(0xffffffffu, last);
+    if (todo) __threadfence();
+    for (; todo; todo &= todo - 1) {
+        const int which = __ffs(todo) - 1, r = which & 15;
+        const int entry = open[which >> 4];
+        const Piece p = pieces[entry >> 1][entry & 1];
+        const int c0 = cta_of(p.first), c1 = cta_of(p.first + p.tiles - 1);
+        Sum x = {-INFINITY, 0.f, {}};
+        constexpr int kBatch = 8;
+        for (int c = c0; c <= c1; c += kBatch) {
+            float pm[kBatch], pl[kBatch], po[kBatch][V], now = x.top;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int cc = min(c + k, c1);
+                const float *part = part_of(cc, p.first < cta_first(cc) ? 0 : 1);  // only the first block has it as its last segment
+                pm[k] = c + k <= c1 ? __ldcg(part + L::kRows * D + r) : -INFINITY;
+                pl[k] = __ldcg(part + L::kRows * D + L::kRows + r);
+                load_o(part + r * D + V * lane, po[k], true);
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) now = fmaxf(now, pm[k]);
+            const float f0 = weight(x.top, now);
+            x.l *= f0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) x.o[i] *= f0;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (c + k > c1) break;
+                const float f = weight(pm[k], now);
+                x.l = fmaf(pl[k], f, x.l);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x.o[i] = fmaf(po[k][i], f, x.o[i]);
+            }
+            x.top = now;
+        }
+        store_out(p, r, x);
     }
 }
 
