@@ -73,11 +73,13 @@ __device__ __forceinline__ void cp_async_wait() {
 __device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return hadd2_u32(prmt(w, 0x64646464u, 0x4140), 0xE480E480u); }
 __device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return hadd2_u32(prmt(w, 0x64646464u, 0x4342), 0xE480E480u); }
 
+// Work is dealt in units: a segment's tiles and, before them, what its beginning and end cost (measured in tiles).
+constexpr int kSegmentCost = 2;
 __device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + kTile - 1) / kTile : 1; }
 
 // A partial result of a segment in a warp's shared memory: which one, and where it starts in the order of all tiles.
 struct Piece {
-    int first;  // the segment's first tile; -1: none
+    int first;  // the unit of the segment's first tile; -1: none
     int tiles, b, head0, rows;
 };
 
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         const int raw = __ldg(a.seq_lens + b), n = length(b);
         if (blockIdx.x == 0 && raw != n) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
         if (b == static_cast<int>(threadIdx.x) * share) first_len = n;
-        sum += tiles_of(n);
+        sum += tiles_of(n) + kSegmentCost;
     }
     int incl = sum;
 #pragma unroll
@@ -149,7 +151,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     const int warp_quota = (cta1 - cta0) / kWarps, warp_more = (cta1 - cta0) % kWarps;
     const int range0 = cta0 + warp * warp_quota + min(warp, warp_more), range1 = range0 + warp_quota + (warp < warp_more ? 1 : 0);
 
-    // Finds the segment of a tile: sequence b, segment s of it, tile i of the segment.
+    // Finds the segment of a unit: sequence b, segment s of it, tile i of the segment (negative: what the segment costs beside its tiles).
     auto locate = [&](int at, int &b, int &s, int &i, int &len) {
         const int seq_tile = at / per_seq;  // a share starts at or before the tile where it starts at or before this
         constexpr int kStep = kThreads / 32;
@@ -158,12 +160,12 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         b = lo * share;
         len = scan_len[lo];
         int rest = at - scan[lo] * per_seq;
-        while (rest >= tiles_of(len) * per_seq && b + 1 < a.n_seqs) {
-            rest -= tiles_of(len) * per_seq;
+        while (rest >= (tiles_of(len) + kSegmentCost) * per_seq && b + 1 < a.n_seqs) {
+            rest -= (tiles_of(len) + kSegmentCost) * per_seq;
             len = length(++b);
         }
-        s = rest / tiles_of(len);
-        i = rest - s * tiles_of(len);
+        s = rest / (tiles_of(len) + kSegmentCost);
+        i = rest - s * (tiles_of(len) + kSegmentCost) - kSegmentCost;
     };
 
     unsigned char *ring = smem + warp * L::kWarp;
@@ -177,11 +179,13 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     if (at < range1) locate(at, b, s, i0, len);
     __syncthreads();
     while (at < range1) {
-        const int n_tiles = tiles_of(len);
+        const int n_tiles = tiles_of(len), first_unit = at - i0;
         const int kvh = s / chunks, chunk = s - kvh * chunks;
         const int head0 = kvh * group + chunk * L::kRows;
         const int rows = min(L::kRows, group - chunk * L::kRows);
-        const int i1 = min(n_tiles, i0 + (range1 - at));
+        const int i1 = min(n_tiles, range1 - first_unit);
+        i0 = max(i0, 0);
+        if (i1 <= i0) break;  // of this segment only the units before its tiles
 
         // lane j holds page and scales of tile base + j (two pages where a page is half a tile)
         int base = i0 - 32;
@@ -447,10 +451,11 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                             *reinterpret_cast<float2 *>(po + r * D + VB * g + 2 * j) = make_float2(o[j][n][k] * ref, o[j][n][k + 2] * ref);
                     }
                 }
-            if (lane == 0) pieces[warp][slot] = {at - i0, n_tiles, b, head0, rows};
+            if (lane == 0) pieces[warp][slot] = {first_unit, n_tiles, b, head0, rows};
         }
-        at += i1 - i0;
-        i0 = 0;
+        if (i1 < n_tiles) break;
+        at = first_unit + n_tiles;
+        i0 = -kSegmentCost;
         if (at < range1 && ++s == per_seq) {
             s = 0;
             len = length(++b);
