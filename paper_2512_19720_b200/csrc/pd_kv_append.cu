@@ -6,16 +6,24 @@
 // with s_held = 0 for a page whose first token is among the new ones.  Both divisions by s' are products with 1 / s'
 // (binary32); a page whose s' is below 2^-120 holds zeros, since 1 / s' would overflow.
 //
-// One thread block takes one (page, head) of the keys or of the values: 16-bit values are read once, kept in registers
-// while the block finds their largest magnitude, and written as codes.  The held codes are read and written again only
-// where the scale grew.  Bound by memory: per value 2 bytes in and 1 byte out (3 with the values handed back).
+// Bound by memory: per value 2 bytes in and 1 byte out (3 with the values handed back).  Two kernels:
+//   pages : a thread block takes one (page, head) of the keys or of the values; the 16-bit values are read once and stay in
+//           registers while the block finds their largest magnitude.  What a block has to know before it can load anything (its
+//           sequence) is one round of loads, the page's number comes with the values.
+//   tokens: a warp takes one (sequence, head) of the keys or of the values and walks over its pages, a token at a time
+//           per half warp.  For decode steps: a block per page would mostly wait for four rounds of loads, and half of the
+//           blocks would find nothing to do (64 sequences of one token, 8 heads of 128: 11.4 against 4.6 us).
+// The held codes are read and written again only where the scale grew.
 #include "pd_attn.cuh"
 #include "pd_ptx.cuh"
 
 namespace pd {
 namespace {
 
-constexpr int kVecs = 8;  // 16-byte pieces (8 values) that a thread keeps in registers
+constexpr int kVecs = 4;         // pages: 16-byte pieces (8 values) that a thread keeps in registers
+constexpr int kMaxThreads = 512;
+constexpr int kTokenWarps = 8;   // tokens: warps of a block
+constexpr int kFewTokens = 4;    // tokens: up to so many new tokens a sequence on average
 
 // max that hands a NaN on, so that a page with a NaN among its values reads as NaN
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -29,27 +37,84 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     return prmt(prmt(static_cast<uint32_t>(x), static_cast<uint32_t>(y), 0x0040), prmt(static_cast<uint32_t>(z), static_cast<uint32_t>(w), 0x0040), 0x5410);
 }
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
+template <bool BF16>
+__device__ __forceinline__ float magnitude(const uint4 &raw, float amax) {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 f = Elem<BF16>::to_float2(w[j]);
+        amax = max_nan(amax, max_nan(fabsf(f.x), fabsf(f.y)));
+    }
+    return amax;
+}
+
+struct Scale {
+    float s, inv;  // 1 / s; 0 where s is too small for it or infinite (a NaN scale gives codes of 0 too)
+};
+__device__ __forceinline__ Scale scale_of(float s_old, float amax) {
+    const float s = max_nan(s_old, __fdiv_rn(amax, 127.f));
+    return {s, s >= 0x1p-120f ? __frcp_rn(s) : 0.f};
+}
+
+// eight values to their codes and, unless nullptr, to the values that those stand for
+template <bool BF16>
+__device__ __forceinline__ void store8(const uint4 &raw, const Scale &sc, int8_t *codes, uint16_t *values) {
     using E = Elem<BF16>;
-    __shared__ float red[8];
-    __shared__ int found;
-    const int id = blockIdx.x, head = blockIdx.y, which = blockIdx.z;
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 t = E::to_float2(w[j]);
+        f[2 * j] = rintf(t.x * sc.inv), f[2 * j + 1] = rintf(t.y * sc.inv);
+    }
+    *reinterpret_cast<uint2 *>(codes) = make_uint2(pack4(f[0], f[1], f[2], f[3]), pack4(f[4], f[5], f[6], f[7]));
+    if (values)
+        *reinterpret_cast<uint4 *>(values) = make_uint4(E::from_float2(f[0] * sc.s, f[1] * sc.s), E::from_float2(f[2] * sc.s, f[3] * sc.s),
+                                                        E::from_float2(f[4] * sc.s, f[5] * sc.s), E::from_float2(f[6] * sc.s, f[7] * sc.s));
+}
+
+// sixteen held codes of the smaller scale to those of the larger one
+__device__ __forceinline__ void scale_again16(uint4 *p, float ratio) {
+    const uint4 c = *p;
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float f[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] = static_cast<float>(static_cast<int8_t>(w[j] >> (8 * k))) * ratio;
+        r[j] = pack4(f[0], f[1], f[2], f[3]);
+    }
+    *p = make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+__device__ __forceinline__ bool bad_lengths(const AppendArgs &a, int first, int last, int len) {
+    return first < 0 || last < first || last > a.n_tokens || len < last - first;
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kMaxThreads, 2) append_pages_kernel(const AppendArgs a) {
+    __shared__ float red[kMaxThreads / 32];
+    const int id = blockIdx.x, head = blockIdx.y, which = blockIdx.z, lane = threadIdx.x & 31;
     const int page = 1 << a.page_log2;
-    // Sequence b's pages are the ids from cu[b] / page + 2 b on: there are never more of them than ids before the next
-    // sequence's, so that the page of a block is found from the offsets alone.
-    if (threadIdx.x == 0) found = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while the previous kernel drains
-    int mine = 0;
-    for (int b = threadIdx.x; b < a.n_seqs; b += blockDim.x)
-        if ((min(max(__ldg(a.cu_seqlens + b), 0), a.n_tokens) >> a.page_log2) + 2 * b <= id) mine = b;  // ascending in b
-    if (mine) atomicMax(&found, mine);
-    __syncthreads();
-    const int b = found;
-    const int first = __ldg(a.cu_seqlens + b), last = __ldg(a.cu_seqlens + b + 1), len = __ldg(a.seq_lens + b);
-    if (first < 0 || last < first || last > a.n_tokens || len < last - first) {
+    // Sequence b's pages are the ids from cu[b] / page + 2 b on: there are never more of them than ids before the next
+    // sequence's.  Every warp finds the last sequence that starts at or before the block's id, 32 candidates a round.
+    int b = 0, n = a.n_seqs, first, last, len;
+    while (true) {
+        const int step = (n + 31) / 32, mine = min(b + lane * step, a.n_seqs - 1);
+        first = __ldg(a.cu_seqlens + mine), last = __ldg(a.cu_seqlens + mine + 1), len = __ldg(a.seq_lens + mine);
+        const unsigned m = __ballot_sync(0xffffffffu, lane * step < n && (min(max(first, 0), a.n_tokens) >> a.page_log2) + 2 * mine <= id);
+        const int src = m ? 31 - __clz(m) : 0;
+        b += src * step;
+        n = min(step, n - src * step);
+        if (n <= 1) {
+            first = __shfl_sync(0xffffffffu, first, src), last = __shfl_sync(0xffffffffu, last, src), len = __shfl_sync(0xffffffffu, len, src);
+            break;
+        }
+    }
+    if (bad_lengths(a, first, last, len)) {
         if (threadIdx.x == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
         return;
     }
@@ -60,6 +125,17 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
     const int hi = static_cast<int>(min(static_cast<int64_t>(len), page_start + page));
     if (lo >= hi) return;
     const int64_t pid = pi < a.table_width ? __ldg(a.block_table + b * a.table_stride + pi) : -1;
+    constexpr int kPer = D / 8;  // pieces of a token
+    const int n_vec = (hi - lo) * kPer;
+    const int64_t tok0 = first + (lo - pos0);
+    const uint16_t *x = static_cast<const uint16_t *>(a.x[which].ptr) + head * a.x[which].head_stride;
+    uint4 raw[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const int at = threadIdx.x + i * blockDim.x;
+        raw[i] = make_uint4(0, 0, 0, 0);
+        if (at < n_vec) raw[i] = __ldg(reinterpret_cast<const uint4 *>(x + (tok0 + at / kPer) * a.x[which].token_stride) + at % kPer);
+    }
     if (pid < 0 || pid >= a.n_pages) {
         if (threadIdx.x == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
         return;
@@ -68,90 +144,100 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
     int8_t *codes = a.pages[which].codes + ((pid * a.kv_heads + head) << a.page_log2) * D;
     float *scale = a.pages[which].scale + pid * a.kv_heads + head;
     const float s_old = held ? *scale : 0.f;
-
-    constexpr int kPer = D / 8;  // pieces of a token
-    const int n_vec = (hi - lo) * kPer;
-    const int64_t tok0 = first + (lo - pos0);
-    const uint16_t *x = static_cast<const uint16_t *>(a.x[which].ptr) + head * a.x[which].head_stride;
-    uint4 raw[kVecs];
     float amax = 0.f;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int at = threadIdx.x + i * blockDim.x;
-        raw[i] = make_uint4(0, 0, 0, 0);
-        if (at < n_vec) raw[i] = __ldg(reinterpret_cast<const uint4 *>(x + (tok0 + at / kPer) * a.x[which].token_stride) + at % kPer);
-    }
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 f = E::to_float2(w[j]);
-            amax = max_nan(amax, max_nan(fabsf(f.x), fabsf(f.y)));
-        }
-    }
+    for (int i = 0; i < kVecs; ++i) amax = magnitude<BF16>(raw[i], amax);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
+    if (lane == 0) red[threadIdx.x >> 5] = amax;
     __syncthreads();
     amax = red[0];
     for (int w = 1; w < static_cast<int>(blockDim.x >> 5); ++w) amax = max_nan(amax, red[w]);
-    const float s_new = max_nan(s_old, __fdiv_rn(amax, 127.f));
-    const float inv = s_new >= 0x1p-120f ? __frcp_rn(s_new) : 0.f;  // 0 for an infinite scale too; a NaN scale gives codes of 0
-
-    if (held && s_new != s_old) {
-        const float ratio = s_old * inv;
-        for (int at = threadIdx.x; at < held * (D / 16); at += blockDim.x) {
-            uint4 *p = reinterpret_cast<uint4 *>(codes) + at;
-            const uint4 c = *p;
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-            uint32_t r[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float f[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) f[k] = static_cast<float>(static_cast<int8_t>(w[j] >> (8 * k))) * ratio;
-                r[j] = pack4(f[0], f[1], f[2], f[3]);
-            }
-            *p = make_uint4(r[0], r[1], r[2], r[3]);
-        }
-    }
+    const Scale sc = scale_of(s_old, amax);
+    if (held && sc.s != s_old)
+        for (int at = threadIdx.x; at < held * (D / 16); at += blockDim.x) scale_again16(reinterpret_cast<uint4 *>(codes) + at, s_old * sc.inv);
     uint16_t *values = static_cast<uint16_t *>(a.values[which]);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        const int at = threadIdx.x + i * blockDim.x;
-        if (at < n_vec) {
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-            float f[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 t = E::to_float2(w[j]);
-                f[2 * j] = rintf(t.x * inv), f[2 * j + 1] = rintf(t.y * inv);
-            }
-            const uint2 c = make_uint2(pack4(f[0], f[1], f[2], f[3]), pack4(f[4], f[5], f[6], f[7]));
-            *(reinterpret_cast<uint2 *>(codes + static_cast<int64_t>(held + at / kPer) * D) + at % kPer) = c;
-            if (values) {
-                const uint4 o = make_uint4(E::from_float2(f[0] * s_new, f[1] * s_new), E::from_float2(f[2] * s_new, f[3] * s_new),
-                                           E::from_float2(f[4] * s_new, f[5] * s_new), E::from_float2(f[6] * s_new, f[7] * s_new));
-                *(reinterpret_cast<uint4 *>(values + ((tok0 + at / kPer) * a.kv_heads + head) * D) + at % kPer) = o;
-            }
-        }
+        const int at = threadIdx.x + i * blockDim.x, tok = at / kPer, piece = at % kPer;
+        if (at < n_vec)
+            store8<BF16>(raw[i], sc, codes + static_cast<int64_t>(held + tok) * D + 8 * piece,
+                         values ? values + ((tok0 + tok) * a.kv_heads + head) * D + 8 * piece : nullptr);
     }
-    if (threadIdx.x == 0) *scale = s_new;
+    if (threadIdx.x == 0) *scale = sc.s;
 }
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kTokenWarps * 32) append_tokens_kernel(const AppendArgs a) {
+    const int lane = threadIdx.x & 31, b = blockIdx.x, item = blockIdx.y * kTokenWarps + (threadIdx.x >> 5);
+    const int which = item & 1, head = item >> 1;
+    const int page = 1 << a.page_log2;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (head >= a.kv_heads) return;
+    const int first = __ldg(a.cu_seqlens + b), last = __ldg(a.cu_seqlens + b + 1), len = __ldg(a.seq_lens + b);
+    if (bad_lengths(a, first, last, len)) {
+        if (lane == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
+        return;
+    }
+    constexpr int kPer = D / 8;       // lanes of a token
+    constexpr int kSide = 32 / kPer;  // tokens side by side
+    const int piece = lane % kPer;
+    const uint16_t *x = static_cast<const uint16_t *>(a.x[which].ptr) + head * a.x[which].head_stride + 8 * piece;
+    uint16_t *values = static_cast<uint16_t *>(a.values[which]);
+    for (int lo = len - (last - first); lo < len;) {
+        const int pi = lo >> a.page_log2, held = lo & (page - 1), n = min(len - lo, page - held);
+        const int64_t tok0 = first + (lo - (len - (last - first)));
+        const int64_t pid = pi < a.table_width ? __ldg(a.block_table + b * a.table_stride + pi) : -1;
+        auto load = [&](int tok) { return __ldg(reinterpret_cast<const uint4 *>(x + (tok0 + tok) * a.x[which].token_stride)); };
+        const int mine = lane / kPer;
+        uint4 raw = make_uint4(0, 0, 0, 0);  // the lane's first token; the others are read twice
+        if (mine < n) raw = load(mine);
+        if (pid < 0 || pid >= a.n_pages) {
+            if (lane == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
+            return;
+        }
+        int8_t *codes = a.pages[which].codes + ((pid * a.kv_heads + head) << a.page_log2) * D;
+        float *scale = a.pages[which].scale + pid * a.kv_heads + head;
+        const float s_old = held ? *scale : 0.f;
+        float amax = magnitude<BF16>(raw, 0.f);
+        for (int tok = mine + kSide; tok < n; tok += kSide) amax = magnitude<BF16>(load(tok), amax);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+        const Scale sc = scale_of(s_old, amax);
+        if (held && sc.s != s_old)
+            for (int at = lane; at < held * (D / 16); at += 32) scale_again16(reinterpret_cast<uint4 *>(codes) + at, s_old * sc.inv);
+        for (int tok = mine; tok < n; tok += kSide) {
+            // in-place values: a token is read for the last time by the lane that then writes it
+            const uint4 v = tok == mine ? raw : *reinterpret_cast<const uint4 *>(x + (tok0 + tok) * a.x[which].token_stride);
+            store8<BF16>(v, sc, codes + static_cast<int64_t>(held + tok) * D + 8 * piece,
+                         values ? values + ((tok0 + tok) * a.kv_heads + head) * D + 8 * piece : nullptr);
+        }
+        if (lane == 0) *scale = sc.s;
+        lo += n;
+    }
+}
+
+using Kernel = void (*)(AppendArgs);
 
 }  // namespace
 
 pd_status launch_kv_append(const AppendArgs &a, bool bf16, cudaStream_t stream) {
     const int page = 1 << a.page_log2;
-    const unsigned ids = static_cast<unsigned>(a.n_tokens / page + 2 * a.n_seqs + 1);
-    const dim3 grid(ids, static_cast<unsigned>(a.kv_heads), 2);
-    const int threads = max(32, min(256, page * a.head_dim / (8 * kVecs)));
-    auto kernel = a.head_dim == 128 ? (bf16 ? kv_append_kernel<128, true> : kv_append_kernel<128, false>)
-                                    : (bf16 ? kv_append_kernel<64, true> : kv_append_kernel<64, false>);
+    const bool few = a.n_tokens <= static_cast<int64_t>(kFewTokens) * a.n_seqs;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    Kernel kernel;
+    if (few) {
+        kernel = a.head_dim == 128 ? (bf16 ? append_tokens_kernel<128, true> : append_tokens_kernel<128, false>)
+                                   : (bf16 ? append_tokens_kernel<64, true> : append_tokens_kernel<64, false>);
+        cfg.gridDim = dim3(static_cast<unsigned>(a.n_seqs), static_cast<unsigned>((2 * a.kv_heads + kTokenWarps - 1) / kTokenWarps));
+        cfg.blockDim = dim3(kTokenWarps * 32);
+    } else {
+        kernel = a.head_dim == 128 ? (bf16 ? append_pages_kernel<128, true> : append_pages_kernel<128, false>)
+                                   : (bf16 ? append_pages_kernel<64, true> : append_pages_kernel<64, false>);
+        cfg.gridDim = dim3(static_cast<unsigned>(a.n_tokens / page + 2 * a.n_seqs), static_cast<unsigned>(a.kv_heads), 2);
+        cfg.blockDim = dim3(static_cast<unsigned>(max(32, page * a.head_dim / (8 * kVecs))));
+    }
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
