@@ -392,39 +392,52 @@ def _heads(t, name, dtype, index):
     return t.data_ptr(), strides[0], strides[1]
 
 
-def _flat(t, name, dtype, index, shape):
-    """Address of a contiguous tensor of a shape."""
+def _refuse(t, name, dtype, index, shape):
+    """Says what is wrong with a tensor that should be contiguous, of a type and of a shape."""
     if t.dtype is not dtype or t.get_device() != index:
         raise TypeError(f"{name} must be a tensor of {dtype} on CUDA device {index}: got {t.dtype} on {t.device}")
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous tensor {tuple(shape)} is wanted: got shape {tuple(t.shape)}, strides {t.stride()}")
+
+
+def _flat(t, name, dtype, index, shape):
+    """Address of a contiguous tensor of a shape."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        _refuse(t, name, dtype, index, shape)
     return t.data_ptr()
 
 
-def _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index):
-    shape = k_codes.shape
+def _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index, seq_lens, block_table, n_seqs):
+    """Checks the cache, its lengths and its table in one expression; returns what the entry points take of them."""
+    shape, table_shape, table_strides = k_codes.shape, block_table.shape, block_table.stride()
+    i8, f32, i32 = torch.int8, torch.float32, torch.int32
     if len(shape) != 4 or (kv_heads is not None and shape[1] != kv_heads) or shape[3] != head_dim:
         raise ValueError(f"k_codes: [pages, kv_heads, page, head_dim] is wanted with {'any' if kv_heads is None else kv_heads} heads of {head_dim}: got {tuple(shape)}")
-    return (_flat(k_codes, "k_codes", torch.int8, index, shape), _flat(v_codes, "v_codes", torch.int8, index, shape),
-            _flat(k_scale, "k_scale", torch.float32, index, shape[:2]), _flat(v_scale, "v_scale", torch.float32, index, shape[:2]), shape[0], shape[2])
-
-
-def _table(seq_lens, block_table, n_seqs, index):
-    shape, strides = block_table.shape, block_table.stride()
-    if block_table.dtype is not torch.int32 or block_table.get_device() != index:
+    if len(table_shape) != 2 or table_shape[0] != n_seqs or (table_strides[1] != 1 and table_shape[1] > 1):
+        raise ValueError(f"block_table: [{n_seqs}, pages of a sequence] with contiguous rows is wanted: got shape {tuple(table_shape)}, strides {table_strides}")
+    scales = shape[:2]
+    if not (k_codes.dtype is i8 and v_codes.dtype is i8 and k_scale.dtype is f32 and v_scale.dtype is f32 and seq_lens.dtype is i32
+            and block_table.dtype is i32 and k_codes.get_device() == index and v_codes.get_device() == index and k_scale.get_device() == index
+            and v_scale.get_device() == index and seq_lens.get_device() == index and block_table.get_device() == index
+            and v_codes.shape == shape and k_scale.shape == scales and v_scale.shape == scales and seq_lens.shape == (n_seqs,)
+            and k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
+            and seq_lens.is_contiguous()):
+        for t, name, dtype, want in ((k_codes, "k_codes", i8, shape), (v_codes, "v_codes", i8, shape), (k_scale, "k_scale", f32, scales),
+                                     (v_scale, "v_scale", f32, scales), (seq_lens, "seq_lens", i32, (n_seqs,))):
+            _refuse(t, name, dtype, index, want)
         raise TypeError(f"block_table must be an int32 tensor on CUDA device {index}: got {block_table.dtype} on {block_table.device}")
-    if len(shape) != 2 or shape[0] != n_seqs or (strides[1] != 1 and shape[1] > 1):
-        raise ValueError(f"block_table: [{n_seqs}, pages of a sequence] with contiguous rows is wanted: got shape {tuple(shape)}, strides {strides}")
-    width = shape[1]
-    return _flat(seq_lens, "seq_lens", torch.int32, index, (n_seqs,)), block_table.data_ptr(), strides[0] if n_seqs > 1 else width, width
+    width = table_shape[1]
+    return (k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0], shape[2], seq_lens.data_ptr(),
+            block_table.data_ptr(), table_strides[0] if n_seqs > 1 else width, width)
 
 
 def _attn_call(name, fn, index, args, workspace):
     """Calls an entry point with `args`, a workspace and the current stream of device `index`."""
-    if torch.cuda.current_device() != index:
+    # what torch.cuda.current_device() and current_stream().cuda_stream return, without their Python objects: 3 us less a call
+    if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return _attn_call(name, fn, index, args, workspace)
-    stream = torch._C._cuda_getCurrentRawStream(index)  # current_stream().cuda_stream without the Python object: 2 us less a call
+    stream = torch._C._cuda_getCurrentRawStream(index)
     if workspace is None:
         _, ptr, size = _attn_workspace(index, stream)
     else:
@@ -467,7 +480,7 @@ def pd_kv_append(k, v, k_codes, v_codes, k_scale, v_scale, cu_seqlens, seq_lens,
     n_tokens, kv_heads, head_dim = shape
     n_seqs = seq_lens.numel()
     args = views + (_flat(cu_seqlens, "cu_seqlens", torch.int32, index, (n_seqs + 1,)), n_seqs, n_tokens, kv_heads, head_dim) + _cache(
-        k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index) + _table(seq_lens, block_table, n_seqs, index) + (
+        k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index, seq_lens, block_table, n_seqs) + (
         None if k_values is None else _flat(k_values, "k_values", dtype, index, shape), None if v_values is None else _flat(v_values, "v_values", dtype, index, shape))
     _attn_call("pd_kv_append", lib.pd_kv_append_bf16 if dtype is torch.bfloat16 else lib.pd_kv_append, index, args, workspace)
 
@@ -482,9 +495,8 @@ def pd_attn_cache(q, k_codes, v_codes, k_scale, v_scale, seq_lens, block_table, 
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != shape:
         raise ValueError(f"out: shape {tuple(out.shape)}, wanted {tuple(shape)}")
-    codes = _cache(k_codes, v_codes, k_scale, v_scale, None, head_dim, index)
-    args = view + (n_seqs, q_heads, k_codes.shape[1], head_dim, head_dim ** -0.5 if scale is None else scale) + codes + _table(
-        seq_lens, block_table, n_seqs, index) + _heads(out, "out", dtype, index)
+    codes = _cache(k_codes, v_codes, k_scale, v_scale, None, head_dim, index, seq_lens, block_table, n_seqs)
+    args = view + (n_seqs, q_heads, k_codes.shape[1], head_dim, head_dim ** -0.5 if scale is None else scale) + codes + _heads(out, "out", dtype, index)
     _attn_call("pd_attn_cache", lib.pd_attn_cache_bf16 if dtype is torch.bfloat16 else lib.pd_attn_cache, index, args, workspace)
     return out
 
