@@ -194,8 +194,19 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = a.q_heads / a.kv_heads;
     const Slots slots = {group % 2 == 0};
-    auto wait = [&](uint64_t *b, uint32_t parity, uint32_t where) { return mbar_wait(b, parity & 1u, abort_flag, a.status, where); };
-    auto wait_warp = [&](uint64_t *b, uint32_t parity, uint32_t where) { return __all_sync(0xffffffffu, wait(b, parity, where)) != 0; };
+    // Bounded; the first one to give up says where, and the block's last act is to report it.  Short, because it is in the code
+    // of every role many times over.
+    auto wait = [&](uint64_t *b, uint32_t parity, int where) {
+        if (mbar_try_wait(b, parity & 1u)) return true;
+        const long long since = clock64();
+        while (!mbar_try_wait(b, parity & 1u))
+            if (clock64() - since > kWaitCycles) {
+                *abort_flag = where;
+                return false;
+            }
+        return true;
+    };
+    auto wait_warp = [&](uint64_t *b, uint32_t parity, int where) { return __all_sync(0xffffffffu, wait(b, parity, where)) != 0; };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) mbar_init(bar.kv_full + i, 1), mbar_init(bar.kv_empty + i, 1);
@@ -243,7 +254,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const int span = slots.by_head ? kTile : 2 * kTile;                     // queries of a unit
             const int per_tile = slots.by_head ? a.q_heads / 2 : a.q_heads;         // units of a tile
             int g0 = -32, first = 0, len = 0, tiles = 0, level = 0, level_base = 0, group_end = 0;
-            uint32_t it = 0, n_diag = 0, n_q[2] = {0, 0};
+            uint32_t it = 0, n_diag = 0, phase_q = 3;  // bit s: slot s; the places are free at first
             bool ok = true;
             int id = blockIdx.x;
             while (ok) {
@@ -289,7 +300,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                         for (int p = 0; p < kPieces; ++p) tma_load_3d(map, full, dst + p * kPieceBytes, p * 64, head, row);
                     };
+#pragma unroll 1
                     for (int j = 0; j < n && ok; ++j) {
+#pragma unroll 1
                         for (int kv = 0; kv < 2 && ok; ++kv, ++it) {
                             const uint32_t st = it % kStages, round = it / kStages;
                             if (round > 0 && !(ok = wait(bar.kv_empty + st, round - 1, 53))) break;
@@ -297,11 +310,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             if (kv == 1 && j >= n0 - 1) full = bar.v_landed + n_diag++ % 4;  // on a diagonal: warp 11 first
                             load(kv == 0 ? &map_k : &map_v, smem + L::kRing + st * L::kTileBytes, full, kvh, u.first + j * kTile);
                             if (j == 0 && kv == 0) {
-#pragma unroll
-                                for (int s = 0; s < 2; ++s) {
-                                    if (!ok || slots.tiles(u, s) == 0) continue;
-                                    if (n_q[s] > 0 && !(ok = wait(bar.q_empty + s, n_q[s] - 1, 52))) continue;
-                                    ++n_q[s];
+#pragma unroll 1
+                                for (int s = 0; s < 2 && ok; ++s) {
+                                    if (slots.tiles(u, s) == 0) continue;
+                                    if (!(ok = wait(bar.q_empty + s, phase_q >> s, 52))) break;
+                                    phase_q ^= 1u << s;
                                     load(&map_q, smem + L::kQ + s * L::kTileBytes, bar.q_full + s, slots.head(u, s), u.first + slots.q0(u, s));
                                 }
                             }
@@ -312,9 +325,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         } else if (warp == 9) {
             // -------------------------------------------------------- S = Q K^T of the units' steps: their slots' tiles in turn
-            constexpr uint32_t kIdesc = kIdescBase<BF16> | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+            const uint32_t idesc = kIdescBase<BF16> | (a.scale < 0.f ? 1u << 13 : 0u) | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);  // bit 13: A negated
             const uint32_t q_desc = desc_lower(smem + L::kQ, 16), k_desc = desc_lower(smem + L::kRing, 16);
-            uint32_t it = 0, n_step = 0, n_q[2] = {0, 0};
+            uint32_t it = 0, n_step = 0, phase_q = 0;  // bit s of a phase: the parity of slot s
             bool ok = true;
             Unit u;
             while (ok && next_unit(u)) {
@@ -325,18 +338,21 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     const uint32_t st = it % kStages;
                     if (!(ok = wait_warp(bar.kv_full + st, it / kStages, 54))) break;
                     const uint32_t k = k_desc + st * (L::kTileBytes >> 4);
-#pragma unroll
+#pragma unroll 1  // the instructions of the roles that run together have to fit into the caches for them
                     for (int s = 0; s < 2; ++s) {
                         const int ns = s ? n1 : n0;
-                        if (!ok || j >= ns) continue;
-                        if (j == 0 && !(ok = wait_warp(bar.q_full + s, n_q[s]++, 55))) continue;
-                        if (n_step > 0 && !(ok = wait_warp(&bar.s_free, n_step - 1, 56))) continue;
+                        if (j >= ns) continue;
+                        if (j == 0) {
+                            if (!(ok = wait_warp(bar.q_full + s, phase_q >> s, 55))) break;
+                            phase_q ^= 1u << s;
+                        }
+                        if (n_step > 0 && !(ok = wait_warp(&bar.s_free, n_step - 1, 56))) break;
                         ++n_step;
                         tcgen05_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
                             const uint32_t off = ((kk / 4) * kPieceBytes + (kk % 4) * 32) >> 4;
-                            mma_smem_a(tmem + kColS, make_desc(q_desc + s * (L::kTileBytes >> 4) + off), make_desc(k + off), kIdesc, kk > 0);
+                            mma_smem_a(tmem + kColS, make_desc(q_desc + s * (L::kTileBytes >> 4) + off), make_desc(k + off), idesc, kk > 0);
                         }
                         commit_elected(bar.s_full + s);
                         if (j + 1 == ns) commit_elected(bar.q_empty + s);
@@ -350,7 +366,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             // -------------------------------------------------------- O += P V of the same steps
             constexpr uint32_t kIdesc = kIdescBase<BF16> | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
             const uint32_t v_desc = desc_lower(smem + L::kRing, kPieceBytes);
-            uint32_t it = 0, n_u[2] = {0, 0}, n_p[2] = {0, 0};
+            uint32_t it = 0, phase_o = 3, phase_p = 0;  // O of each slot is free at first
             bool ok = true;
             Unit u;
             while (ok && next_unit(u)) {
@@ -360,20 +376,24 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     const uint32_t st = (it + 1) % kStages;
                     if (!(ok = wait_warp(bar.kv_full + st, (it + 1) / kStages, 57))) break;
                     const uint32_t v = v_desc + st * (L::kTileBytes >> 4);
-#pragma unroll
+#pragma unroll 1
                     for (int s = 0; s < 2; ++s) {
-                        if (!ok || j >= (s ? n1 : n0)) continue;
-                        if (j == 0 && n_u[s]++ > 0 && !(ok = wait_warp(bar.o_empty + s, n_u[s] - 2, 58))) continue;
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            if (!ok || !(ok = wait_warp(bar.p_half[s] + half, n_p[s], 60))) continue;
-                            tcgen05_fence_after();
-#pragma unroll
-                            for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
-                                mma_tmem_a(tmem + kColO + s * 128, tmem + kColP + s * 64 + kk * 8, make_desc(v + kk * (2048 >> 4)), kIdesc, (j > 0 || kk > 0) ? 1u : 0u);
+                        if (j >= (s ? n1 : n0)) continue;
+                        if (j == 0) {
+                            if (!(ok = wait_warp(bar.o_empty + s, phase_o >> s, 58))) break;
+                            phase_o ^= 1u << s;
                         }
-                        if (!ok) continue;
-                        ++n_p[s];
+#pragma unroll 1
+                        for (int half = 0; half < 2 && ok; ++half) {
+                            if (!(ok = wait_warp(bar.p_half[s] + half, phase_p >> s, 60))) break;
+                            tcgen05_fence_after();
+                            const uint32_t v_half = v + half * (4 * 2048 >> 4), p_half = tmem + kColP + s * 64 + half * 32;
+#pragma unroll
+                            for (int kk = 0; kk < 4; ++kk)
+                                mma_tmem_a(tmem + kColO + s * 128, p_half + kk * 8, make_desc(v_half + kk * (2048 >> 4)), kIdesc, (j + half + kk > 0) ? 1u : 0u);
+                        }
+                        if (!ok) break;
+                        phase_p ^= 1u << s;
                         commit_elected(bar.o_done + s);
                     }
                     if (ok) commit_elected(bar.kv_empty + st);
@@ -429,8 +449,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const uint32_t ts = lanes + kColS, tp = lanes + kColP + s * 64, to = lanes + kColO + s * 128;
-        const float scale2 = a.scale * kLog2e;
-        const float f = scale2 > 0.f ? scale2 : (scale2 < 0.f ? -scale2 : 1.f);
+        // The maximum is taken before the scores are scaled, so that the factor is positive: the products give -Q K^T for a
+        // negative scale, and a scale of zero is one that makes nothing of any finite score (minus infinity stays what it is).
+        const float f = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1e-30f;
         uint32_t n_s = 0;  // tiles of the slot so far
         bool ok = true;
         Unit u;
@@ -445,6 +466,19 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             for (int j = 0; j < n; ++j, ++n_s) {
                 if (!(ok = wait_warp(bar.s_full + s, n_s, 60))) break;
                 tcgen05_fence_after();
+                if (j == n - 1) {  // on the diagonal: keys 0 .. r of the tile; in place and in a loop, which keeps the code short
+#pragma unroll 1
+                    for (int c = r & ~31; c < kTile; c += 32) {
+                        uint32_t y[32];
+                        tcgen05_ld_32x32b_x32(ts + c, y);
+                        tcgen05_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (c + k > r) y[k] = 0xff800000u;
+                        tcgen05_st_32x32b_x32(ts + c, y);
+                    }
+                    tcgen05_wait_st();
+                }
                 uint32_t x[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tcgen05_ld_32x32b_x32(ts + 32 * c, x[c]);
@@ -452,19 +486,6 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bar.s_free);
-                if (scale2 <= 0.f) {  // the maximum is taken before the scores are scaled by |scale|
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) x[c][k] = scale2 < 0.f ? x[c][k] ^ 0x80000000u : __float_as_uint(__uint_as_float(x[c][k]) * 0.f);
-                }
-                if (j == n - 1) {  // on the diagonal: keys 0 .. r of the tile
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (32 * c + k > r) x[c][k] = __float_as_uint(-INFINITY);
-                }
                 float top[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -576,6 +597,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     tcgen05_fence_before();
     __syncthreads();
     if (*abort_flag) {
+        if (threadIdx.x == 0) latch_error(a.status, PD_ERR_DEVICE_TIMEOUT, static_cast<uint32_t>(*abort_flag));
         for (int i = 0; i < 64; ++i) __nanosleep(10000);  // copies that may still be in flight
         __syncthreads();
     }
