@@ -113,22 +113,25 @@ __device__ __forceinline__ bool non_finite2(uint32_t w) {
 __device__ __forceinline__ void mma_smem_a(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n"
-        ".reg .pred p, q;\n"
+        ".reg .pred p;\n"
         "setp.ne.b32 p, %4, 0;\n"
-        "elect.sync _|q, 0xffffffff;\n"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
         "}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 __device__ __forceinline__ void mma_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n"
-        ".reg .pred p, q;\n"
+        ".reg .pred p;\n"
         "setp.ne.b32 p, %4, 0;\n"
-        "elect.sync _|q, 0xffffffff;\n"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
         "}\n" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t x;
+    asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xffffffff;\nselp.b32 %0, 1, 0, q;\n}\n" : "=r"(x));
+    return x != 0;
 }
 __device__ __forceinline__ void commit_elected(uint64_t *bar) {
     asm volatile(
@@ -349,6 +352,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         if (n_step > 0 && !(ok = wait_warp(&bar.s_free, n_step - 1, 56))) break;
                         ++n_step;
                         tcgen05_fence_after();
+                        if (elect_one())
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
                             const uint32_t off = ((kk / 4) * kPieceBytes + (kk % 4) * 32) >> 4;
@@ -388,6 +392,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             if (!(ok = wait_warp(bar.p_half[s] + half, phase_p >> s, 60))) break;
                             tcgen05_fence_after();
                             const uint32_t v_half = v + half * (4 * 2048 >> 4), p_half = tmem + kColP + s * 64 + half * 32;
+                            if (elect_one())
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk)
                                 mma_tmem_a(tmem + kColO + s * 128, p_half + kk * 8, make_desc(v_half + kk * (2048 >> 4)), kIdesc, (j + half + kk > 0) ? 1u : 0u);
