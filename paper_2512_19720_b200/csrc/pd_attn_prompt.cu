@@ -7,6 +7,9 @@
 //
 // Bound by the tensor cores (4 * head_dim operations per query, key and head) and, as nearly, by the exponentials: a tile of
 // 128 x 128 scores is 1024 clocks of products at head_dim 128 and 1024 clocks of the 16 exponentials a clock that an SM has.
+// Measured: 64 query and 8 key/value heads of 128, one prompt of 8192 tokens 0.93-0.97 ms, 1.1-1.2 PFLOP/s at the power limit
+// (a polynomial for some of the exponentials changed nothing); 7 prompts of 7919 tokens together 222 us; 32 heads, 4 prompts of 512
+// tokens 24 us, where what surrounds the products counts: first loads, the last units of the blocks, instructions not in the cache.
 //
 // A block works on units of two *slots* of 128 queries each that read the same keys: two heads that share their key/value
 // head where their number is even, else two consecutive pieces of one head's queries.  Tiles of 128 keys: S = Q K^T (both
@@ -15,14 +18,15 @@
 // are computed.
 // Tensor memory: one buffer of 128 columns for S that both slots use in turn (a row of S is taken into registers at once, and
 // the buffer is free again long before its softmax is done), 64 columns of P and 128 of O for each slot.  So the scores of a
-// slot's next tile wait for its softmax, not the softmax for them.  With a buffer of S for each slot and P in its place, a
-// slot's softmax stood still during its own two products: 64 query heads, 8192 tokens 1110 us.
+// slot's next tile wait for its softmax, not the softmax for them.  (A buffer of S for each slot with P in its place, where a
+// slot's softmax stands still during its own two products: 1110 us where this gave 900.)
 //
-// Roles: warps 0-3 and 4-7 the softmax and the output of slot 0 and 1; warp 8 units and TMA; warps 9 and 10 issue the
-// products with the keys and with the values (one warp for both was kept from one by its waits for the other); warp 11
-// looks for infinities and NaN among the values of a tile on the diagonal, where 0 * v must not reach the
-// queries that do not attend to v: they are set to zero there, and the output adds them for the queries that do.  A tile on
-// the diagonal is full for the products when it has been through it.  Every wait is bounded.
+// Roles: warps 0-3 and 4-7 the softmax of slot 0 and 1; warp 8 units and TMA; warps 9 and 10 issue the products with the
+// keys and with the values (one warp for both, scores first: 20 % slower); warp 11 looks for infinities and NaN among the
+// values of a tile on the diagonal, where 0 * v must not reach the queries that do not attend to v: they are set to zero
+// there, and the output adds them for the queries that do (a tile on the diagonal is full for the products when warp 11 has
+// been through it); warps 12-15 write the output while the softmax is at the next unit.  Every wait is bounded.
+// The code is kept short on purpose: at 92 KB of instructions a warp in two waited for its next one.
 #include "pd_attn.cuh"
 #include "pd_tcgen05.cuh"
 
@@ -30,7 +34,7 @@ namespace pd {
 namespace {
 
 constexpr int kTile = 128;  // queries of a slot, keys of a tile
-constexpr int kWarps = 12;
+constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
 constexpr int kUnits = 4;  // units that the producer may be ahead
 constexpr float kLog2e = 1.4426950408889634f;
@@ -57,9 +61,10 @@ struct PromptSmem {
     static constexpr int kStages = D == 128 ? 4 : 8;  // of keys or values
     static constexpr int kQ = 0;
     static constexpr int kRing = 2 * kTileBytes;
-    static constexpr int kOut = kRing + kStages * kTileBytes;  // for each softmax warp 32 rows of 32 outputs
-    static constexpr int kBars = kOut + 8 * 32 * 64;
-    static constexpr int kTotal = kBars + 1024 + 1024;  // + slack for 1024-byte alignment
+    static constexpr int kOut = kRing + kStages * kTileBytes;  // for each output warp 32 rows of outputs
+    static constexpr int kSums = kOut + 4 * 32 * D * 2;          // l of the two slots' rows, for two units
+    static constexpr int kBars = kSums + 2 * 2 * kTile * 4;
+    static constexpr int kTotal = kBars + 512;
     static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
@@ -67,14 +72,14 @@ struct Bars {
     uint64_t kv_full[8], kv_empty[8];
     uint64_t v_landed[4];  // tiles on a diagonal, in turn: no more of them are in the ring
     uint64_t q_full[2], q_empty[2];
-    uint64_t s_full[2], s_free, p_half[2][2], o_done[2], o_empty[2];
+    uint64_t s_full[2], s_free, p_half[2][2], o_done[2], o_last[2], o_empty[2];
     uint64_t unit_full[kUnits], unit_empty[kUnits];
     Unit units[kUnits];
     int taint[kUnits];
     uint32_t tmem;
     int abort_flag;
 };
-static_assert(sizeof(Bars) <= 1024, "barriers");
+static_assert(sizeof(Bars) <= 512, "barriers");
 
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -107,9 +112,9 @@ __device__ __forceinline__ bool non_finite2(uint32_t w) {
     return (w & e) == e || ((w >> 16) & e) == e;
 }
 
-// The products and their commits are written for a whole warp of which one elected thread acts: inside `if (lane == 0)` the
-// compiler moved every operand of every instruction to the uniform registers anew, and the issue of a 64-clock product took
-// 105 clocks.
+// The products of a group are issued inside `if (elect_one())` by a warp whose other threads keep to the same path: inside
+// `if (lane == 0)` the compiler moved every operand of every instruction to the uniform registers anew (105 clocks for the
+// issue of a 64-clock product), and with an election for each of them a product took 39 instructions instead of 5.
 __device__ __forceinline__ void mma_smem_a(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n"
@@ -117,15 +122,6 @@ __device__ __forceinline__ void mma_smem_a(uint32_t d_tmem, uint64_t a_desc, uin
         "setp.ne.b32 p, %4, 0;\n"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
         "}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-__device__ __forceinline__ void mma_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n"
-        ".reg .pred p;\n"
-        "setp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
-        "}\n" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 __device__ __forceinline__ bool elect_one() {
@@ -190,8 +186,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     static_assert(kStages % 2 == 0, "keys and values keep to their own stages");
     constexpr int kPieces = D / 64;                    // sub-tiles of 64 columns
     constexpr int kPieceBytes = kTile * 64 * 2;
-    extern __shared__ unsigned char smem_raw[];
-    unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    extern __shared__ __align__(1024) unsigned char smem[];  // the swizzle counts from 1024-byte boundaries
     Bars &bar = *reinterpret_cast<Bars *>(smem + L::kBars);
     volatile int *abort_flag = &bar.abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -217,10 +212,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         for (int s = 0; s < 2; ++s) {
             mbar_init(bar.q_full + s, 1), mbar_init(bar.q_empty + s, 1), mbar_init(bar.s_full + s, 1);
             mbar_init(bar.p_half[s], 4), mbar_init(bar.p_half[s] + 1, 4), mbar_init(bar.o_done + s, 1);
-            mbar_init(bar.o_empty + s, 4);
+            mbar_init(bar.o_last + s, 1), mbar_init(bar.o_empty + s, 4);
         }
         mbar_init(&bar.s_free, 4);
-        for (int i = 0; i < kUnits; ++i) mbar_init(bar.unit_full + i, 1), mbar_init(bar.unit_empty + i, 11);
+        for (int i = 0; i < kUnits; ++i) mbar_init(bar.unit_full + i, 1), mbar_init(bar.unit_empty + i, 15);
         bar.abort_flag = 0;
         mbar_fence_init();
     }
@@ -246,8 +241,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         ++n_unit;
     };
 
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp >= 8 && warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 8) {
             // -------------------------------------------------------- units and TMA
             // Units in the order of their work, most first, so that the blocks end together: the last queries of every sequence
@@ -395,11 +390,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             if (elect_one())
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk)
-                                mma_tmem_a(tmem + kColO + s * 128, p_half + kk * 8, make_desc(v_half + kk * (2048 >> 4)), kIdesc, (j + half + kk > 0) ? 1u : 0u);
+                                tcgen05_mma_f16_tmem_a(tmem + kColO + s * 128, p_half + kk * 8, make_desc(v_half + kk * (2048 >> 4)), kIdesc, (j + half + kk > 0) ? 1u : 0u);
                         }
                         if (!ok) break;
                         phase_p ^= 1u << s;
                         commit_elected(bar.o_done + s);
+                        if (j + 1 == (s ? n1 : n0)) commit_elected(bar.o_last + s);
                     }
                     if (ok) commit_elected(bar.kv_empty + st);
                 }
@@ -447,8 +443,61 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 done_unit();
             }
         }
+    } else if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // ------------------------------------------------------------ output: O / l of both slots, while the softmax is at the next unit
+        const int w = warp & 3;
+        uint32_t n_sum[2] = {0, 0};
+        bool ok = true;
+        Unit u;
+        while (ok && next_unit(u)) {
+#pragma unroll 1
+            for (int s = 0; s < 2; ++s) {
+                if (slots.tiles(u, s) == 0) continue;
+                const uint32_t k_u = s ? n_sum[1]++ : n_sum[0]++;
+                if (!(ok = wait_warp(bar.o_last + s, k_u, 62))) break;
+                tcgen05_fence_after();
+                const float inv = 1.f / reinterpret_cast<const float *>(smem + L::kSums)[((k_u & 1) * 2 + s) * kTile + w * 32 + lane];
+                const uint32_t to = tmem + (static_cast<uint32_t>(w * 32) << 16) + kColO + s * 128;
+                // Rows go through shared memory, so that O is free as soon as it has been read, and they leave in whole lines:
+                // written by the threads that own them they were 32 pieces of 16 bytes an instruction.
+                constexpr int kRow = D * 2, kPer = D / 8;  // bytes and 16-byte pieces of a row
+                unsigned char *out = smem + L::kOut + w * (32 * kRow);
+#pragma unroll
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t o[16];
+                    tcgen05_ld_32x32b_x16(to + c, o);
+                    tcgen05_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = E::from_float2(__uint_as_float(o[8 * k + 2 * i]) * inv, __uint_as_float(o[8 * k + 2 * i + 1]) * inv);
+                        *reinterpret_cast<uint4 *>(out + lane * kRow + (((c / 8 + k) ^ (lane & 7)) * 16)) = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
+                }
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.o_empty + s);
+                const int head = slots.head(u, s), row0 = slots.q0(u, s) + w * 32;  // the warp's first row
+                const int piece = lane % kPer, rows = min(32, u.len - row0);
+                uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0 + lane / kPer) * a.out.token_stride +
+                              head * a.out.head_stride + 8 * piece;
+#pragma unroll 4
+                for (int i = lane / kPer; i < rows; i += 32 / kPer, y += (32 / kPer) * a.out.token_stride)
+                    *reinterpret_cast<uint4 *>(y) = *reinterpret_cast<const uint4 *>(out + i * kRow + ((piece ^ (i & 7)) * 16));
+                __syncwarp();
+                if (bar.taint[n_unit % kUnits] && lane < rows)
+                    add_non_finite<BF16>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0 + lane) * a.out.token_stride +
+                                             head * a.out.head_stride, D,
+                                         static_cast<const uint16_t *>(a.v.ptr) + static_cast<int64_t>(u.first + u.q0) * a.v.token_stride +
+                                             (head / group) * a.v.head_stride, a.v.token_stride, row0 + lane - u.q0 + 1);
+            }
+            if (!ok) break;
+            done_unit();
+        }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         // ------------------------------------------------------------ softmax and output: a thread owns one row of a slot
         const int s = warp >> 2;
         const int r = (warp & 3) * 32 + lane;
@@ -457,7 +506,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // The maximum is taken before the scores are scaled, so that the factor is positive: the products give -Q K^T for a
         // negative scale, and a scale of zero is one that makes nothing of any finite score (minus infinity stays what it is).
         const float f = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1e-30f;
-        uint32_t n_s = 0;  // tiles of the slot so far
+        uint32_t n_s = 0, n_sum = 0;  // tiles and units of the slot so far
         bool ok = true;
         Unit u;
         while (ok && next_unit(u)) {
@@ -500,7 +549,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * f;
                 // Before O is rescaled or P written the product with the tile before has to be done.
-                bool may_write = j == 0;
+                bool may_write = n_s == 0;
                 auto until_done = [&]() {
                     if (!may_write) {
                         may_write = wait_warp(bar.o_done + s, n_s - 1, 61);
@@ -551,49 +600,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 quarter(x[2], p1);  // while the first half is stored
                 hand_over(0);
                 quarter(x[3], p1 + 16);
+                // l goes to the warps that write the output.  They have read what is there from the unit before the last: P of this
+                // unit could only be written after a product that waited for them.
+                if (j == n - 1) reinterpret_cast<float *>(smem + L::kSums)[((n_sum & 1) * 2 + s) * kTile + r] = l.x + l.y;
                 tcgen05_st_32x32b_x32(tp + 32, p1);
                 hand_over(1);
             }
             if (!ok) break;
-            if (!(ok = wait_warp(bar.o_done + s, n_s - 1, 62))) break;
-            tcgen05_fence_after();
-            const float inv = 1.f / (l.x + l.y);
-            const int head = slots.head(u, s), row0 = slots.q0(u, s) + (warp & 3) * 32;  // the warp's first row
-            // Rows go through shared memory, so that they leave in pieces of 64 bytes: written by the threads that own them
-            // they were 32 pieces of 16 bytes an instruction.
-            unsigned char *out = smem + L::kOut + warp * (32 * 64);
-            const int piece = lane & 3;
-            uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0 + (lane >> 2)) * a.out.token_stride +
-                          head * a.out.head_stride + 8 * piece;
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                tcgen05_ld_32x32b_x32(to + c, o);
-                tcgen05_wait_ld();
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint32_t x[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = E::from_float2(__uint_as_float(o[8 * k + 2 * i]) * inv, __uint_as_float(o[8 * k + 2 * i + 1]) * inv);
-                    *reinterpret_cast<uint4 *>(out + lane * 64 + ((k ^ ((lane >> 1) & 3)) * 16)) = make_uint4(x[0], x[1], x[2], x[3]);
-                }
-                if (c + 32 == D) tcgen05_fence_before();
-                __syncwarp();
-                if (c + 32 == D && lane == 0) mbar_arrive(bar.o_empty + s);  // O has been read
-                uint16_t *row = y + c;
-#pragma unroll
-                for (int k = 0; k < 4; ++k, row += 8 * a.out.token_stride) {
-                    const int i = 8 * k + (lane >> 2);
-                    const uint4 x = *reinterpret_cast<const uint4 *>(out + i * 64 + ((piece ^ ((i >> 1) & 3)) * 16));
-                    if (row0 + i < u.len) *reinterpret_cast<uint4 *>(row) = x;
-                }
-                __syncwarp();
-            }
-            if (bar.taint[n_unit % kUnits] && row0 + lane < u.len)
-                add_non_finite<BF16>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(u.first + row0 + lane) * a.out.token_stride +
-                                         head * a.out.head_stride, D,
-                                     static_cast<const uint16_t *>(a.v.ptr) + static_cast<int64_t>(u.first + u.q0) * a.v.token_stride +
-                                         (head / group) * a.v.head_stride, a.v.token_stride, row0 + lane - u.q0 + 1);
+            ++n_sum;
             done_unit();
         }
     }
