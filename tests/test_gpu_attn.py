@@ -90,9 +90,10 @@ def test_prompt_rising_and_falling_scores(api):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_prompt_what_is_not_attended_to_has_no_influence(api, dtype, bad):
+@pytest.mark.parametrize("hkv,d", [(2, 128), (4, 128), (2, 64), (4, 64)])
+def test_prompt_what_is_not_attended_to_has_no_influence(api, hkv, d, dtype, bad):
     lens = [70, 130, 33]
-    q, k, v = prompt_inputs(lens, 4, 2, 128, dtype, 11)
+    q, k, v = prompt_inputs(lens, 4, hkv, d, dtype, 11)
     clean = api.pd_attn_prompt(q, k, v, offsets(lens))
     k2, v2 = k.clone(), v.clone()
     k2[65:70], v2[65:70] = bad, bad   # the last tokens of the first sequence
@@ -100,9 +101,10 @@ def test_prompt_what_is_not_attended_to_has_no_influence(api, dtype, bad):
     got = api.pd_attn_prompt(q, k2, v2, offsets(lens))
     keep = torch.ones_like(got, dtype=torch.bool)
     keep[65:70] = False
-    keep[170:200, 2:, 5] = False
+    heads = slice(4 // hkv, 8 // hkv)  # those that read key/value head 1
+    keep[170:200, heads, 5] = False
     assert torch.equal(got[keep], clean[keep])
-    hit = got[170:200, 2:, 5].float()
+    hit = got[170:200, heads, 5].float()
     assert bool(torch.isnan(hit).all() if bad != bad else (hit == bad).all())
     assert bool(torch.isnan(got[65:70].float()).any())
 
@@ -137,10 +139,10 @@ def test_prompt_bad_offsets_are_reported(api):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_prompt_long_sequences_on_samples(api, dtype):
+@pytest.mark.parametrize("hq,hkv,d", [(16, 4, 128), (12, 12, 128), (18, 6, 64)])
+def test_prompt_long_sequences_on_samples(api, hq, hkv, d, dtype):
     """Thousands of tokens, many heads, next to short sequences: sampled queries against 64-bit sums."""
     lens = [2500, 3, 1111, 640]
-    hq, hkv, d = 16, 4, 128
     q, k, v = prompt_inputs(lens, hq, hkv, d, dtype, 19)
     got = api.pd_attn_prompt(q, k, v, offsets(lens))
     rng = np.random.default_rng(3)
@@ -152,6 +154,26 @@ def test_prompt_long_sequences_on_samples(api, dtype):
             close(f64(got[at + i]), f64(torch.einsum("hj,jhd->hd", w, vs)), f64(torch.einsum("hj,jhd->hd", w, vs.abs())), UNIT[dtype], UNIT[dtype],
                   2.0 ** -25 * n * 5 if dtype == torch.float16 else 0.0)
         at += n
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (3, 3, 128)])
+def test_prompt_many_sequences(api, hq, hkv, d):
+    """More sequences than the lanes of a warp know at a time, some of them empty, some longer than a tile."""
+    rng = np.random.default_rng(127)
+    lens = [int(n) for n in rng.choice([0, 1, 2, 7, 31, 130], 75)]
+    q, k, v = prompt_inputs(lens, hq, hkv, d, torch.float16, 131)
+    got = api.pd_attn_prompt(q, k, v, offsets(lens))
+    assert api.pd_device_status(api.attn_workspace()) == 0
+    check_prompt(got, q, k, v, lens, d ** -0.5, torch.float16)
+
+
+def test_prompt_again_and_again_gives_the_same_bits(api):
+    """The blocks take their work in the order in which they come to it: the results do not depend on it."""
+    lens = [700, 1300, 40, 511]
+    q, k, v = prompt_inputs(lens, 16, 4, 128, torch.bfloat16, 137)
+    first = api.pd_attn_prompt(q, k, v, offsets(lens))
+    for _ in range(20):
+        assert torch.equal(first, api.pd_attn_prompt(q, k, v, offsets(lens)))
 
 
 # ------------------------------------------------------------------ the cache
@@ -211,7 +233,7 @@ def test_cache_attention_matches_the_definition(api, hq, hkv, d, page, dtype):
 
 
 @pytest.mark.parametrize("lens", [[1], [5], [333], [7, 9000], [20011]], ids=str)
-@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 128), (16, 2, 64), (32, 2, 128)])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 128), (16, 2, 64), (32, 2, 128), (16, 1, 128), (1, 1, 64)])
 def test_cache_attention_split_over_blocks(api, lens, hq, hkv, d):
     """Few rows: the work of a sequence is cut into parts that are joined."""
     page = 64
