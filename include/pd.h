@@ -431,7 +431,8 @@ pd_status pd_kv_append_bf16(const void *k, int64_t k_token_stride, int64_t k_hea
  *   out : out, [n_seqs, q_heads, head_dim] = softmax(scale q . K^T, over the seq_lens[b] cached tokens) . V; zeros where
  *         seq_lens[b] is 0
  * Slots of a page past the sequence's end and pages that it does not reach have no influence, whatever they hold.
- * Parts of a long sequence are joined in a fixed order: the same call gives the same bits.
+ * Parts of a long sequence are joined in a fixed order: the same call gives the same bits.  n_seqs * q_heads * (table_width *
+ * page / 16 + 1) must stay below 2^30, table_width * page too.
  */
 pd_status pd_attn_cache(const void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n_seqs, int32_t q_heads,
                         int32_t kv_heads, int32_t head_dim, float scale, const int8_t *k_codes, const int8_t *v_codes,

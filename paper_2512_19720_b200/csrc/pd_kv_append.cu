@@ -20,8 +20,8 @@
 namespace pd {
 namespace {
 
-constexpr int kVecs = 4;         // pages: 16-byte pieces (8 values) that a thread keeps in registers
-constexpr int kMaxThreads = 512;
+constexpr int kVecs = 8;         // pages: 16-byte pieces (8 values) that a thread keeps in registers
+constexpr int kMaxThreads = 256;
 constexpr int kTokenWarps = 8;   // tokens: warps of a block
 constexpr int kFewTokens = 4;    // tokens: up to so many new tokens a sequence on average
 
@@ -98,7 +98,7 @@ __device__ __forceinline__ bool bad_lengths(const AppendArgs &a, int first, int 
 }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kMaxThreads, 3) append_pages_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 4) append_pages_kernel(const AppendArgs a) {
     __shared__ float red[kMaxThreads / 32];
     const int id = blockIdx.x, head = blockIdx.y, which = blockIdx.z, lane = threadIdx.x & 31;
     const int page = 1 << a.page_log2;
@@ -106,15 +106,15 @@ __global__ void __launch_bounds__(kMaxThreads, 3) append_pages_kernel(const Appe
     asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while the previous kernel drains
     // Sequence b's pages are the ids from cu[b] / page + 2 b on: there are never more of them than ids before the next
     // sequence's.  Every warp finds the last sequence that starts at or before the block's id, 32 candidates a round.
-    int b = 0, n = a.n_seqs, first, last, len;
+    int b = 0, left = a.n_seqs, first, last, len;
     while (true) {
-        const int step = (n + 31) / 32, mine = min(b + lane * step, a.n_seqs - 1);
+        const int step = (left + 31) / 32, mine = min(b + lane * step, a.n_seqs - 1);
         first = __ldg(a.cu_seqlens + mine), last = __ldg(a.cu_seqlens + mine + 1), len = __ldg(a.seq_lens + mine);
-        const unsigned m = __ballot_sync(0xffffffffu, lane * step < n && (min(max(first, 0), a.n_tokens) >> a.page_log2) + 2 * mine <= id);
+        const unsigned m = __ballot_sync(0xffffffffu, lane * step < left && (min(max(first, 0), a.n_tokens) >> a.page_log2) + 2 * mine <= id);
         const int src = m ? 31 - __clz(m) : 0;
         b += src * step;
-        n = min(step, n - src * step);
-        if (n <= 1) {
+        left = min(step, left - src * step);
+        if (left <= 1) {
             first = __shfl_sync(0xffffffffu, first, src), last = __shfl_sync(0xffffffffu, last, src), len = __shfl_sync(0xffffffffu, len, src);
             break;
         }
@@ -131,15 +131,15 @@ __global__ void __launch_bounds__(kMaxThreads, 3) append_pages_kernel(const Appe
     if (lo >= hi) return;
     const int64_t pid = pi < a.table_width ? __ldg(a.block_table + b * a.table_stride + pi) : -1;
     constexpr int kPer = D / 8;  // pieces of a token
-    const int n_vec = (hi - lo) * kPer;
-    const int64_t tok0 = first + (lo - pos0);
-    const uint16_t *x = static_cast<const uint16_t *>(a.x[which].ptr) + head * a.x[which].head_stride;
+    const int n = hi - lo, tok = threadIdx.x / kPer, piece = threadIdx.x % kPer, stride = blockDim.x / kPer;  // a thread takes every stride-th token's piece
+    const int64_t tok0 = first + (lo - pos0) + tok;
+    const uint16_t *x = static_cast<const uint16_t *>(a.x[which].ptr) + head * a.x[which].head_stride + tok0 * a.x[which].token_stride + 8 * piece;
     uint4 raw[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        const int at = threadIdx.x + i * blockDim.x;
         raw[i] = make_uint4(0, 0, 0, 0);
-        if (at < n_vec) raw[i] = __ldg(reinterpret_cast<const uint4 *>(x + (tok0 + at / kPer) * a.x[which].token_stride) + at % kPer);
+        if (tok + i * stride < n) raw[i] = __ldg(reinterpret_cast<const uint4 *>(x));
+        x += stride * a.x[which].token_stride;
     }
     if (pid < 0 || pid >= a.n_pages) {
         if (threadIdx.x == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
@@ -160,14 +160,13 @@ __global__ void __launch_bounds__(kMaxThreads, 3) append_pages_kernel(const Appe
     const Scale sc = scale_of(s_old, amax);
     if (held && sc.s != s_old)
         for (int at = threadIdx.x; at < held * (D / 16); at += blockDim.x) scale_again16(reinterpret_cast<uint4 *>(codes) + at, s_old * sc.inv);
+    int8_t *to = codes + (held + tok) * D + 8 * piece;
     uint16_t *values = static_cast<uint16_t *>(a.values[which]);
+    if (values) values += (tok0 * a.kv_heads + head) * D + 8 * piece;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int at = threadIdx.x + i * blockDim.x, tok = at / kPer, piece = at % kPer;
-        if (at < n_vec)
-            store8<BF16>(raw[i], sc, codes + static_cast<int64_t>(held + tok) * D + 8 * piece,
-                         values ? values + ((tok0 + tok) * a.kv_heads + head) * D + 8 * piece : nullptr);
-    }
+    for (int i = 0; i < kVecs; ++i)
+        if (tok + i * stride < n)
+            store8<BF16>(raw[i], sc, to + i * stride * D, values ? values + static_cast<int64_t>(i * stride) * a.kv_heads * D : nullptr);
     if (threadIdx.x == 0) *scale = sc.s;
 }
 
