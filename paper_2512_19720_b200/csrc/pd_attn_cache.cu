@@ -31,6 +31,9 @@ constexpr int kMaxGrid = 1024;
 constexpr int kMaxRows = 16;    // heads of a segment
 constexpr size_t kCounterBytes = kMaxGrid * kMaxRows * 4;  // for each block and row: parts of the segment that goes on behind the block
 constexpr float kLog2e = 1.4426950408889634f;
+// A sum that starts from the bits of 1.5 * 2^23 is, read as binary32, that number and the sum (below 2^22 in magnitude).
+constexpr float kShift = 12582912.f;
+constexpr int kShiftBits = 0x4B400000;
 constexpr float kMaxLead = 8.f;         // how far (base-2 exponent) a score may pass the reference maximum
 
 template <int D, int NT>
@@ -69,6 +72,13 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+// 16 tokens x 32 dimensions of codes against 32 dimensions x 8 heads of signed bytes
+__device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 // bytes (0, 1) or (2, 3) of w (each a code ^ 0x80) as two binary16 codes
 __device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return hadd2_u32(prmt(w, 0x64646464u, 0x4140), 0xE480E480u); }
 __device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return hadd2_u32(prmt(w, 0x64646464u, 0x4342), 0xE480E480u); }
@@ -92,7 +102,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     using L = CacheShape<D, NT>;
     constexpr int kWarps = L::kWarps, kThreads = L::kThreads, kStages = L::kStages;
     constexpr int MT = D / 16;      // 16-row products of O^T
-    constexpr int KS = D / 16;      // contraction steps of S
+    constexpr int KS = D / 32;      // contraction steps of S
     constexpr int KC = D / 64;      // 16-byte pieces of a key that a thread takes
     constexpr int VB = D / 8;       // bytes of a value that a thread takes
     extern __shared__ __align__(16) unsigned char smem[];
@@ -250,7 +260,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         }
         float o[MT][NT][4];
         float m[NT][2], mu[NT][2], l[NT][2], qs[NT][2];
-        uint32_t qf[KS][NT][2];
+        uint32_t qf[KS][NT][3][2];
         float ref = 0.f;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -260,7 +270,8 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                 for (int k = 0; k < 4; ++k) o[i][n][k] = 0.f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            // the head's query, scaled by a power of two to a largest magnitude of 1..2: exact in binary16 for both types
+            // The head's query as whole numbers of 23 bits, in three signed bytes: multiples of 2^-21 of the power of two
+            // below its largest magnitude.
             const int r = n * 8 + g;
             float x[KC][16], amax = 0.f;
 #pragma unroll
@@ -284,16 +295,31 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
             // 2^-e with e the exponent of amax, held to what binary32 and its reciprocal can say
             const int e = min(max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100), 100);
             const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+            float bad = 0.f;  // NaN where the query has an infinity or a NaN
 #pragma unroll
             for (int c = 0; c < KC; ++c)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    qf[c * 4 + k][n][0] = Elem<false>::from_float2(x[c][4 * k] * down, x[c][4 * k + 1] * down);
-                    qf[c * 4 + k][n][1] = Elem<false>::from_float2(x[c][4 * k + 2] * down, x[c][4 * k + 3] * down);
+                    uint32_t byte[3] = {0u, 0u, 0u};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        bad = fmaf(x[c][4 * k + i], 0.f, bad);
+                        int rest = __float2int_rn(x[c][4 * k + i] * down * 0x1p21f);
+#pragma unroll
+                        for (int j = 0; j < 3; ++j) {
+                            const int low = static_cast<int8_t>(rest);
+                            byte[j] |= (static_cast<uint32_t>(low) & 0xffu) << (8 * i);
+                            rest = (rest - low) >> 8;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) qf[c * 2 + k / 2][n][j][k & 1] = byte[j];
                 }
+            bad += __shfl_xor_sync(0xffffffffu, bad, 1);
+            bad += __shfl_xor_sync(0xffffffffu, bad, 2);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                qs[n][k] = lscale * __shfl_sync(0xffffffffu, up, (2 * t + k) * 4);
+                qs[n][k] = lscale * __shfl_sync(0xffffffffu, up * 0x1p-21f + bad, (2 * t + k) * 4);
                 m[n][k] = -INFINITY, mu[n][k] = 0.f, l[n][k] = 0.f;
             }
         }
@@ -311,24 +337,35 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                 float acc[2][NT][4];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    int part[NT][3][4];
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[h][n][k] = 0.f;
+                        for (int j = 0; j < 3; ++j)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) part[n][j][k] = kShiftBits;
 #pragma unroll
                     for (int c = 0; c < KC; ++c) {
                         const int row = 16 * h + g, piece = D == 128 ? (t + 4 * c) ^ ((row & 1) * 4) : t;
                         const uint4 lo = *reinterpret_cast<const uint4 *>(ks + row * D + piece * 16);
                         const uint4 hi = *reinterpret_cast<const uint4 *>(ks + (row + 8) * D + piece * 16);
-                        const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int j = 0; j < 3; ++j) {
+                                mma_s8(part[n][j], lo.x, hi.x, lo.y, hi.y, qf[c * 2][n][j][0], qf[c * 2][n][j][1]);
+                                mma_s8(part[n][j], lo.z, hi.z, lo.w, hi.w, qf[c * 2 + 1][n][j][0], qf[c * 2 + 1][n][j][1]);
+                            }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const uint32_t ul = wl[k] ^ 0x80808080u, uh = wh[k] ^ 0x80808080u;
-                            const uint32_t a0 = codes_lo(ul), a1 = codes_lo(uh), a2 = codes_hi(ul), a3 = codes_hi(uh);
+                            float f[3];
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) Elem<false>::mma16816(acc[h][n], a0, a1, a2, a3, qf[c * 4 + k][n][0], qf[c * 4 + k][n][1]);
+                            for (int j = 0; j < 3; ++j) f[j] = __int_as_float(part[n][j][k]) - kShift;
+                            acc[h][n][k] = fmaf(f[2], 65536.f, fmaf(f[1], 256.f, f[0]));
                         }
-                    }
                 }
                 // scores in base 2; places past the end of the sequence are chosen away, whatever they hold
                 bool lead = false;
