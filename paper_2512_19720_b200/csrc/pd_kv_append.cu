@@ -20,7 +20,9 @@
 namespace pd {
 namespace {
 
-constexpr int kVecs = 8;         // pages: 16-byte pieces (8 values) that a thread keeps in registers
+// pages: 16-byte pieces (8 values) that a thread keeps in registers; 8523 tokens, 8 heads of 128, pages of 64: 18.0 us with 4,
+// 16.9 with 8, of which the bytes (88 MB) take 13.5
+constexpr int kVecs = 8;
 constexpr int kMaxThreads = 256;
 constexpr int kTokenWarps = 8;   // tokens: warps of a block
 constexpr int kFewTokens = 4;    // tokens: up to so many new tokens a sequence on average
