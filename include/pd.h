@@ -363,7 +363,7 @@ pd_status pd_fit_layer(const void *x_tr, const void *y_tr, int64_t M_tr, const v
  *
  * Cache.  Pages of `page` (16, 32, 64 or 128) consecutive tokens of one sequence: codes int8
  * [n_pages, kv_heads, page, head_dim] and scales fp32 [n_pages, kv_heads], for keys and for values.  A code c of a page
- * and head with scale s stands for c * s.  block_table int32 [n_seqs, table_stride] (device): entry i of sequence b is
+ * and head with scale s >= 0 stands for c * s, where s is below 2^-120 for 0.  block_table int32 [n_seqs, table_stride] (device): entry i of sequence b is
  * the page of its tokens i * page .. (i + 1) * page; only the entries that its length reaches are read, of at most
  * table_width.  seq_lens int32 [n_seqs] (device): tokens of each sequence, for pd_kv_append AFTER the call, so that the
  * append and the attention behind it take the same lengths.

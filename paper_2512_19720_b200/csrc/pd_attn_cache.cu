@@ -23,7 +23,7 @@
 // Softmax in base 2 with 32-bit statistics.  The reference maximum m of a head and the reference scale r of V move only
 // when a score passes m by more than 8 or a page's scale leaves [r / 8, 8 r]: P is rounded to binary16 as
 // 2^(s - m) * (page scale / r) <= 2^11, so that its relative precision does not depend on how stale m and r are, and O
-// needs no multiplication at most tiles.
+// needs no multiplication at most tiles.  r falls with the page scales as far as O, which is kept in units of r, stays in range.
 #include "pd_attn.cuh"
 #include "pd_ptx.cuh"
 
@@ -39,6 +39,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kShift = 12582912.f;
 constexpr int kShiftBits = 0x4B400000;
 constexpr float kMaxLead = 8.f;         // how far (base-2 exponent) a score may pass the reference maximum
+constexpr float kSmallestScale = 0x1p-120f;  // a page of V whose scale is below it counts as zeros; so 1 / r is finite
+constexpr float kMostOutput = 0x1p100f;      // O, in units of r, stays below about this where r falls; what r does not follow is 2^-100 of O
 
 template <int D, int NT>
 struct CacheShape {
@@ -255,7 +257,8 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                         }
                     }
                 }
-                if (lane == src) meta[st] = make_float4(sk[0], sk[1], sv[0], sv[1]);  // after the copies: the scales may still be on their way
+                if (lane == src)  // after the copies: the scales may still be on their way
+                    meta[st] = make_float4(sk[0], sk[1], sv[0] < kSmallestScale ? 0.f : sv[0], sv[1] < kSmallestScale ? 0.f : sv[1]);
             }
             cp_async_commit();
         };
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         float o[MT][NT][4];
         float m[NT][2], mu[NT][2], l[NT][2], qs[NT][2];
         uint32_t qf[KS][NT][3][2];
-        float ref = 0.f;
+        float ref = 0.f, inv_ref = 0.f, ref_top = 0.f;  // the reference scale of V, its reciprocal, and the largest that O was summed with
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -389,8 +392,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                 const float sv_hi = fmaxf(sc.z, sc.w);
                 const bool move_ref = sv_hi > 8.f * ref || (sv_hi < 0.125f * ref && sv_hi > 0.f);
                 if (__any_sync(0xffffffffu, lead) || move_ref) {
-                    const float step = move_ref ? ref / sv_hi : 1.f;
-                    if (move_ref) ref = sv_hi;
+                    float factor[NT][2];  // for O
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -400,15 +402,41 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                             for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
                             top = fmaxf(top, m[n][k]);
                             const float mu_new = top == -INFINITY ? 0.f : top;
-                            const float shrink = exp2_approx(m[n][k] - mu_new);  // 0 from -infinity on
-                            l[n][k] *= shrink;
+                            factor[n][k] = exp2_approx(m[n][k] - mu_new);  // 0 from -infinity on
+                            l[n][k] *= factor[n][k];
                             m[n][k] = top, mu[n][k] = mu_new;
-                            const float f = shrink * step;
-#pragma unroll
-                            for (int j = 0; j < MT; ++j) o[j][n][k] *= f, o[j][n][k + 2] *= f;
                         }
+                    if (move_ref) {
+                        float step = ref / sv_hi;
+                        if (sv_hi < ref_top * 0x1p-60f) {
+                            // far below the largest r that O was summed with: r follows as long as O stays in range
+                            float most = 0.f;
+#pragma unroll
+                            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) most = fmaxf(most, fabsf(o[j][n][k] * factor[n][k & 1]));
+#pragma unroll
+                            for (int d = 1; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+                            step = most > 0.f ? fmaxf(fminf(step, kMostOutput / most), 1.f) : 1.f;
+                            ref = most > 0.f ? fmaxf(sv_hi, ref / step) : sv_hi;
+                            if (most == 0.f) ref_top = 0.f;
+                        } else {
+                            ref = sv_hi;
+                        }
+                        ref_top = fmaxf(ref_top, ref);
+                        inv_ref = __frcp_rn(ref);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) factor[n][0] *= step, factor[n][1] *= step;
+                    }
+#pragma unroll
+                    for (int j = 0; j < MT; ++j)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[j][n][k] *= factor[n][k & 1];
                 }
-                const float inv_ref = ref > 0.f ? __frcp_rn(ref) : 0.f;
                 const float rv[2] = {sc.z == 0.f ? 0.f : sc.z * inv_ref, sc.w == 0.f ? 0.f : sc.w * inv_ref};
                 uint32_t pf[2][NT][2];
 #pragma unroll

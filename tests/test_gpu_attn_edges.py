@@ -1,0 +1,130 @@
+"""Attention operators on the GPU at the ends of their ranges, against fp64 definitions.
+
+Bound of pd_attn_cache, for each output, with w_j the weights and M the largest score of the row, L = sum_j e^(s_j - M):
+  - rounding to the output's type: u_out |out| (u = 2^-11 for binary16, 2^-8 for bfloat16), and its smallest step;
+  - P in binary16: 2^-11 sum_j w_j |v_j|; where P is subnormal 2^-25 of a unit, which is at most 8 page scales of the tile and at
+    most 1 / L of a weight: 2^-22 / L sum_j (largest page scale of j's tile) |code_j|;
+  - scores: a query is a multiple of 2^-21 of the power of two below its largest value, so that a score is off by
+    d_j <= scale 2^-22 max|q| sum |k_j|; binary32 arithmetic adds 2^-20 (|s_j| + 1).  Weights are off by e^(2 max d) - 1 then."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pd_oracle_attn as orc
+
+pytestmark = pytest.mark.gpu
+UNIT = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+SMALLEST = {torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133}
+TYPES = [torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def api():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    from paper_2512_19720_b200 import api
+    return api
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def offsets(lens):
+    return i32(np.concatenate([[0], np.cumsum(lens)]).tolist())
+
+
+class Cache:
+    """Pages of some sequences, one after another: codes int8 [pages, heads, page, d], scales [pages, heads]; numpy arrays."""
+
+    def __init__(self, lens, hkv, d, page, seed):
+        self.lens, self.page = lens, page
+        rng = np.random.default_rng(seed)
+        n = [-(-x // page) for x in lens]
+        self.table, at = np.full((len(lens), max(n)), -1), 0
+        for b, m in enumerate(n):
+            self.table[b, :m] = np.arange(at, at + m)
+            at += m
+        self.k_codes, self.v_codes = (rng.integers(-127, 128, (at, hkv, page, d)).astype(np.int8) for _ in range(2))
+        self.k_scale, self.v_scale = (np.exp(rng.normal(-4, 0.3, (at, hkv))).astype(np.float32) for _ in range(2))
+
+    def device(self):
+        return [torch.from_numpy(x).cuda() for x in (self.k_codes, self.v_codes, self.k_scale, self.v_scale)] + [i32(self.lens), i32(self.table.tolist())]
+
+    def rows(self, b, g):
+        """Codes of K and V and the scales of each token of sequence b, head g (fp64); V's scales below 2^-120 count as zero."""
+        n, pages = self.lens[b], self.table[b, :-(-self.lens[b] // self.page)]
+        flat = lambda x: x[pages, g].reshape(-1, x.shape[3])[:n].astype(np.float64)  # noqa: E731
+        each = lambda x: np.repeat(x[pages, g].astype(np.float64), self.page)[:n]  # noqa: E731
+        sv = each(self.v_scale)
+        return flat(self.k_codes), flat(self.v_codes), each(self.k_scale), np.where(sv < 2.0 ** -120, 0.0, sv)
+
+    def definition(self, q, scale, dtype):
+        """Outputs and their bound for queries q (fp64) [B, Hq, d]."""
+        out, bound = np.zeros_like(q), np.zeros_like(q)
+        group = q.shape[1] // self.k_codes.shape[1]
+        for b in range(len(self.lens)):
+            for h in range(q.shape[1] if self.lens[b] else 0):
+                kc, vc, sk, sv = self.rows(b, h // group)
+                s = (kc @ q[b, h]) * sk * scale
+                e = np.exp(s - s.max())
+                w = e / e.sum()
+                v = vc * sv[:, None]
+                tile = np.arange(len(s)) // 32
+                tile_scale = np.maximum.reduceat(sv, np.arange(0, len(s), 32))[tile]
+                off = (abs(scale) * 2.0 ** -22 * np.abs(q[b, h]).max() * np.abs(kc).sum(1) * sk + 2.0 ** -20 * (np.abs(s) + 1)).max()
+                near = w @ np.abs(v)
+                out[b, h] = w @ v
+                bound[b, h] = (UNIT[dtype] * np.abs(out[b, h]) + SMALLEST[dtype] + (2.0 ** -11 + np.expm1(2 * off)) * near +
+                               2.0 ** -22 / e.sum() * (tile_scale @ np.abs(vc)))
+        return out, bound
+
+
+def check(got, want, bound):
+    got = f64(got)
+    assert np.all(np.isfinite(got))
+    assert np.all(np.abs(got - want) <= bound), float((np.abs(got - want) / bound).max())
+
+
+def attend(api, cache, q, scale):
+    got = api.pd_attn_cache(q, *cache.device(), scale)
+    assert api.pd_device_status(api.attn_workspace()) == 0
+    return got
+
+
+# ------------------------------------------------------------------ scales of V at the ends of their range
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (12, 1, 64), (4, 4, 64)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_cache_values_with_scales_of_any_size(api, hq, hkv, d, page):
+    """Pages of V that are below 2^-120 (zeros), just above it, or far above or below the others, in every order."""
+    n = 12 * page + 3
+    scales = [[2.0 ** -126] * 13, [1e-38, 1.0] + [1e-38] * 11, [1.0] * 6 + [2.0 ** -119] * 7, [2.0 ** -119] * 6 + [1.0] * 7, [3e4] * 8 + [1e-36] * 5,
+              [2.0 ** (16 * (6 - i)) for i in range(13)], [2.0 ** (16 * (i - 6)) for i in range(13)], [1.0, 0.0, 2.0 ** -100, 0.0] * 3 + [1.0]]
+    cache = Cache([n] * len(scales), hkv, d, page, 5)
+    for b, of_pages in enumerate(scales):
+        cache.v_scale[cache.table[b]] = np.array(of_pages, dtype=np.float32)[:, None]
+    q = torch.randn(len(scales), hq, d, generator=torch.Generator("cuda").manual_seed(hq), device="cuda").bfloat16()
+    want, bound = cache.definition(f64(q), d ** -0.5, torch.bfloat16)
+    check(attend(api, cache, q, d ** -0.5), want, bound)
+    assert not want[0].any() and np.median(bound[1:5] / np.abs(want[1:5])) < 0.05
+
+
+def test_appended_values_that_are_tiny(api):
+    """What pd_kv_append writes for values near 1e-38 reads as zeros, before, after and without ordinary pages."""
+    d, page, n = 64, 32, 96
+    gen = torch.Generator("cuda").manual_seed(9)
+    k, q = torch.randn(n, 1, d, generator=gen, device="cuda").bfloat16(), torch.randn(1, 2, d, generator=gen, device="cuda").bfloat16()
+    for tiny in ([0, 1, 2], [0], [1], [2]):
+        v = torch.ones(n, 1, d, dtype=torch.bfloat16, device="cuda")
+        for i in tiny:
+            v[i * page:(i + 1) * page] = 1e-38
+        tensors = [torch.zeros(3, 1, page, d, dtype=torch.int8, device="cuda") for _ in range(2)] + [torch.zeros(3, 1, device="cuda") for _ in range(2)]
+        api.pd_kv_append(k, v, *tensors, offsets([n]), i32([n]), i32([[0, 1, 2]]))
+        got = f64(api.pd_attn_cache(q, *tensors, i32([n]), i32([[0, 1, 2]])))
+        cache = Cache([n], 1, d, page, 0)
+        cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale = (t.cpu().numpy() for t in tensors)
+        want, bound = cache.definition(f64(q), d ** -0.5, torch.bfloat16)
+        assert np.all(np.abs(got - want) <= bound) and (len(tiny) < 3 or not got.any())
