@@ -35,9 +35,9 @@ constexpr int kMaxGrid = 1024;
 constexpr int kMaxRows = 16;    // heads of a segment
 constexpr size_t kCounterBytes = kMaxGrid * kMaxRows * 4;  // for each block and row: parts of the segment that goes on behind the block
 constexpr float kLog2e = 1.4426950408889634f;
-// A sum that starts from the bits of 1.5 * 2^23 is, read as binary32, that number and the sum (below 2^22 in magnitude).
-constexpr float kShift = 12582912.f;
-constexpr int kShiftBits = 0x4B400000;
+// A sum that starts from the bits of 1.5 * 2^2 is, read as binary32, that number and 2^-21 of the sum (below 2^22 in magnitude).
+constexpr float kShift = 6.f;
+constexpr int kShiftBits = 0x40C00000;
 constexpr float kMaxLead = 8.f;         // how far (base-2 exponent) a score may pass the reference maximum
 constexpr float kSmallestScale = 0x1p-120f;  // a page of V whose scale is below it counts as zeros; so 1 / r is finite
 constexpr float kMostOutput = 0x1p100f;      // O, in units of r, stays below about this where r falls; what r does not follow is 2^-100 of O
@@ -279,8 +279,9 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                 for (int k = 0; k < 4; ++k) o[i][n][k] = 0.f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            // The head's query as whole numbers of 23 bits, in three signed bytes: multiples of 2^-21 of the power of two
-            // below its largest magnitude.
+            // The head's query as whole numbers of 23 bits, in three signed bytes: multiples of 2^-21 of the power of two 2^e
+            // below its largest magnitude.  That is exact for values down to 2^-11 of the largest (2^-14 in bfloat16); smaller ones
+            // are off by up to 2^-22 of the largest, four times what binary32 loses of a sum that the largest takes part in.
             const int r = n * 8 + g;
             float x[KC][16], amax = 0.f;
 #pragma unroll
@@ -301,9 +302,10 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
             }
             amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
             amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            // 2^-e with e the exponent of amax, held to what binary32 and its reciprocal can say
-            const int e = min(max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100), 100);
-            const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+            // 2^(21 - e) for every e that binary32 has, in two factors
+            const int e = min(max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -126), 127), half = (21 - e) >> 1;
+            const float down0 = __uint_as_float(static_cast<uint32_t>(127 + half) << 23);
+            const float down1 = __uint_as_float(static_cast<uint32_t>(127 + 21 - e - half) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
             float bad = 0.f;  // NaN where the query has an infinity or a NaN
 #pragma unroll
             for (int c = 0; c < KC; ++c)
@@ -313,12 +315,11 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         bad = fmaf(x[c][4 * k + i], 0.f, bad);
-                        int rest = __float2int_rn(x[c][4 * k + i] * down * 0x1p21f);
+                        int rest = __float2int_rn(x[c][4 * k + i] * down0 * down1);
 #pragma unroll
                         for (int j = 0; j < 3; ++j) {
-                            const int low = static_cast<int8_t>(rest);
-                            byte[j] |= (static_cast<uint32_t>(low) & 0xffu) << (8 * i);
-                            rest = (rest - low) >> 8;
+                            byte[j] |= (static_cast<uint32_t>(rest) & 0xffu) << (8 * i);
+                            rest = (rest >> 8) + ((rest >> 7) & 1);  // less the signed byte
                         }
                     }
 #pragma unroll
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
             bad += __shfl_xor_sync(0xffffffffu, bad, 2);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                qs[n][k] = lscale * __shfl_sync(0xffffffffu, up * 0x1p-21f + bad, (2 * t + k) * 4);
+                qs[n][k] = lscale * __shfl_sync(0xffffffffu, up + bad, (2 * t + k) * 4);
                 m[n][k] = -INFINITY, mu[n][k] = 0.f, l[n][k] = 0.f;
             }
         }

@@ -128,3 +128,42 @@ def test_appended_values_that_are_tiny(api):
         cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale = (t.cpu().numpy() for t in tensors)
         want, bound = cache.definition(f64(q), d ** -0.5, torch.bfloat16)
         assert np.all(np.abs(got - want) <= bound) and (len(tiny) < 3 or not got.any())
+
+
+# ------------------------------------------------------------------ queries of any size
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (12, 1, 64)])
+def test_cache_queries_at_the_ends_of_bfloat16(api, hq, hkv, d):
+    """A query times a power of two with the scale divided by it gives the same bits, from the smallest normal exponent to the largest."""
+    cache = Cache([70, 333, 1], hkv, d, 32, 11)
+    gen = torch.Generator("cuda").manual_seed(13)
+    q = torch.rand(3, hq, d, generator=gen, device="cuda").bfloat16() * 0.984375 + 1.0  # magnitudes in [1, 2)
+    assert float(q.min()) >= 1 and float(q.max()) < 2
+    q *= torch.randint(0, 2, q.shape, generator=gen, device="cuda").bfloat16() * 2 - 1
+    for scale, powers in ((2.0 ** -3, (-101, -113, -120, -126)), (16.0, (99, 101, 102, 103, 110, 125, 127))):
+        if scale > 1:
+            cache.k_scale *= np.float32(2.0 ** -7)
+        clean = attend(api, cache, q, scale)
+        want, bound = cache.definition(f64(q), scale, torch.bfloat16)
+        check(clean, want, bound)
+        for e in powers:
+            big = (q.double() * 2.0 ** e).bfloat16()
+            assert torch.equal(big.double(), q.double() * 2.0 ** e)
+            assert torch.equal(attend(api, cache, big, scale * 2.0 ** -e), clean), e
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        big = q.clone()
+        big[1, 0, 7] = bad
+        got = attend(api, cache, big, 2.0 ** -3)
+        assert bool(torch.isnan(got[1, 0]).all()) and bool(torch.isfinite(got[1, 1:]).all()) and bool(torch.isfinite(got[0]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("factor", [2.0 ** 6, 2.0 ** 9])
+def test_cache_query_with_one_large_channel(api, dtype, factor):
+    """Most of a head's query is far below its largest value; the keys hardly use that channel, so that the rest decides."""
+    cache = Cache([500, 90], 2, 128, 64, 17)
+    cache.k_codes[..., 5] = np.sign(cache.k_codes[..., 5])
+    q = torch.randn(2, 4, 128, generator=torch.Generator("cuda").manual_seed(19), device="cuda").to(dtype)
+    q[..., 5] = factor
+    want, bound = cache.definition(f64(q), 0.3, dtype)
+    assert np.median(bound) < 0.04 * np.sqrt(np.mean(want ** 2))
+    check(attend(api, cache, q, 0.3), want, bound)
