@@ -370,7 +370,7 @@ pd_status pd_fit_layer(const void *x_tr, const void *y_tr, int64_t M_tr, const v
  *
  * Workspace: pd_workspace_bytes(PD_OP_ATTN, 0, 0, 0, 0) bytes that are all zero before the first call.  Every call leaves
  * its status words and counters as the next one needs them; calls queued on one stream can share it, calls that overlap
- * on the GPU and calls of other operations need workspaces of their own.
+ * on the GPU (of graphs that are replayed side by side too) and calls of other operations need workspaces of their own.
  * Errors that only the device sees (offsets or lengths out of range, a page number outside [0, n_pages)) latch
  * PD_ERR_BAD_INDEX; nothing outside the given tensors is read or written, and what that sequence gets is unspecified.
  */
@@ -452,6 +452,13 @@ const char *pd_status_string(pd_status status);
 
 /* Number of kernels the library has launched in this process since load (for accounting). */
 int64_t pd_launch_count(void);
+
+/*
+ * The capture into a CUDA graph that cuda_stream takes part in (a number that no other capture of the process has), 0 if
+ * it is not being captured.  Scratch memory that has to start from zero must not be shared between graphs, whose replays
+ * may come in any order: this says which graph a call goes into.
+ */
+uint64_t pd_capture_id(void *cuda_stream);
 
 #ifdef __cplusplus
 }

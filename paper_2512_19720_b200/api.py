@@ -20,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpd.so")
 
 EXPORTS = ["pd_pack_delta", "pd_pack_delta_static", "pd_linear_host", "pd_linear", "pd_linear_ex", "pd_linear_multivariant", "pd_merge",
-           "pd_workspace_bytes", "pd_device_status", "pd_status_string", "pd_launch_count", "pd_selftest_bounded_wait",
+           "pd_workspace_bytes", "pd_device_status", "pd_status_string", "pd_launch_count", "pd_capture_id", "pd_selftest_bounded_wait",
            "pd_pack_delta_bf16", "pd_merge_bf16", "pd_linear_bf16", "pd_linear_multivariant_bf16",
            "pd_artifact_bytes", "pd_load_merged",
            "pd_transpose_mask", "pd_fit_loss_grad", "pd_fit_adamw_step", "pd_fit_layer",
@@ -95,6 +95,8 @@ def _load() -> ctypes.CDLL:
             fn.argtypes, fn.restype = argtypes, ctypes.c_int
     lib.pd_launch_count.argtypes = []
     lib.pd_launch_count.restype = i64
+    lib.pd_capture_id.argtypes = [p]
+    lib.pd_capture_id.restype = ctypes.c_uint64
     for name, proto in (("pd_pack_delta_bf16", lib.pd_pack_delta), ("pd_merge_bf16", lib.pd_merge),
                         ("pd_linear_bf16", lib.pd_linear_ex), ("pd_linear_multivariant_bf16", lib.pd_linear_multivariant)):
         fn = getattr(lib, name)
@@ -363,23 +365,31 @@ def pd_fit_layer(x_tr, y_tr, x_val, y_val, w_b, mask, v_row0, v_col0, epochs, ba
 
 # The attention calls are short (a few microseconds on the GPU), so that their binding looks at each tensor once.
 _attn_ws_cache: dict = {}
+_attn_graph_ws: dict = {}
 _HALF_TYPES = (torch.float16, torch.bfloat16)
+# what torch.cuda.current_device(), current_stream().cuda_stream and is_current_stream_capturing() return, without their
+# Python objects: 3 us less a call
+_get_device, _raw_stream, _capturing = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch._C._cuda_isCurrentStreamCapturing
 
 
 def _attn_workspace(index: int, stream: int):
     """The attention calls' own scratch tensor with its address and size, one for each device and stream: it must be all
-    zero before its first call, and calls that overlap on the GPU must not share it."""
-    ws = _attn_ws_cache.get((index, stream))
-    if ws is None:
+    zero before its first call, and calls that overlap on the GPU must not share it.  Calls that are captured get one of
+    their graph's own, since graphs are replayed in any order and on any stream: each replay zeroes it first."""
+    capture = lib.pd_capture_id(stream) if stream else 0  # the default stream cannot be captured
+    cache = _attn_graph_ws if capture else _attn_ws_cache
+    ws = cache.get((index, stream))
+    if ws is None or ws[3] != capture:
         t = torch.zeros(workspace_bytes(OP_ATTN), dtype=torch.uint8, device=torch.device("cuda", index))
-        ws = _attn_ws_cache[index, stream] = (t, t.data_ptr(), t.numel())
+        ws = cache[index, stream] = (t, t.data_ptr(), t.numel(), capture)
     return ws
 
 
 def attn_workspace(device=None) -> torch.Tensor:
-    """The workspace that attention calls without one of their own use on the current stream (for pd_device_status)."""
+    """The workspace that attention calls without one of their own use on the current stream (for pd_device_status).  A
+    captured graph's own is zeroed at every replay, its status too: give a workspace to calls whose status is to be read."""
     index = torch.cuda.current_device() if device is None or device.index is None else device.index
-    return _attn_workspace(index, torch._C._cuda_getCurrentRawStream(index))[0]
+    return _attn_workspace(index, _raw_stream(index))[0]
 
 
 def _heads(t, name, dtype, index):
@@ -433,13 +443,13 @@ def _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index, seq_le
 
 def _attn_call(name, fn, index, args, workspace):
     """Calls an entry point with `args`, a workspace and the current stream of device `index`."""
-    # what torch.cuda.current_device() and current_stream().cuda_stream return, without their Python objects: 3 us less a call
-    if torch._C._cuda_getDevice() != index:
+    if _get_device() != index:
         with torch.cuda.device(index):
             return _attn_call(name, fn, index, args, workspace)
-    stream = torch._C._cuda_getCurrentRawStream(index)
+    stream = _raw_stream(index)
     if workspace is None:
-        _, ptr, size = _attn_workspace(index, stream)
+        ws = None if stream and _capturing() else _attn_ws_cache.get((index, stream))
+        _, ptr, size, _ = ws or _attn_workspace(index, stream)
     else:
         ptr, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     code = fn(*args, ptr, size, stream)

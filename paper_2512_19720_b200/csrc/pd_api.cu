@@ -198,6 +198,16 @@ const char *pd_status_string(pd_status s) {
 
 int64_t pd_launch_count(void) { return g_launches.load(); }
 
+uint64_t pd_capture_id(void *cuda_stream) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (cudaStreamGetCaptureInfo(static_cast<cudaStream_t>(cuda_stream), &status, &id) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    return status == cudaStreamCaptureStatusNone ? 0 : id;
+}
+
 }  // extern "C"
 
 namespace {
