@@ -371,8 +371,9 @@ pd_status pd_fit_layer(const void *x_tr, const void *y_tr, int64_t M_tr, const v
  * Workspace: pd_workspace_bytes(PD_OP_ATTN, 0, 0, 0, 0) bytes that are all zero before the first call.  Every call leaves
  * its status words and counters as the next one needs them; calls queued on one stream can share it, calls that overlap
  * on the GPU (of graphs that are replayed side by side too) and calls of other operations need workspaces of their own.
- * Errors that only the device sees (offsets or lengths out of range, a page number outside [0, n_pages)) latch
- * PD_ERR_BAD_INDEX; nothing outside the given tensors is read or written, and what that sequence gets is unspecified.
+ * Errors that only the device sees (offsets or lengths out of range, offsets that decrease, a page number outside
+ * [0, n_pages)) latch PD_ERR_BAD_INDEX; nothing outside the given tensors is read or written, and what that sequence gets is
+ * unspecified; where offsets decrease, what every sequence of the call gets.
  */
 
 /*

@@ -106,6 +106,11 @@ __global__ void __launch_bounds__(kMaxThreads, 4) append_pages_kernel(const Appe
     const int page = 1 << a.page_log2;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while the previous kernel drains
+    if (head == 0 && which == 0) {  // offsets that decrease may keep the search below from ever seeing a sequence: the first blocks look at all
+        const int64_t b = static_cast<int64_t>(id) * blockDim.x + threadIdx.x;
+        if (b < a.n_seqs && bad_lengths(a, __ldg(a.cu_seqlens + b), __ldg(a.cu_seqlens + b + 1), __ldg(a.seq_lens + b)))
+            latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
+    }
     // Sequence b's pages are the ids from cu[b] / page + 2 b on: there are never more of them than ids before the next
     // sequence's.  Every warp finds the last sequence that starts at or before the block's id, 32 candidates a round.
     int b = 0, left = a.n_seqs, first, last, len;
@@ -121,10 +126,7 @@ __global__ void __launch_bounds__(kMaxThreads, 4) append_pages_kernel(const Appe
             break;
         }
     }
-    if (bad_lengths(a, first, last, len)) {
-        if (threadIdx.x == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
-        return;
-    }
+    if (bad_lengths(a, first, last, len)) return;
     const int pos0 = len - (last - first);  // position of the first new token
     const int pi = (pos0 >> a.page_log2) + id - ((first >> a.page_log2) + 2 * b);
     const int64_t page_start = static_cast<int64_t>(pi) << a.page_log2;

@@ -167,3 +167,33 @@ def test_cache_query_with_one_large_channel(api, dtype, factor):
     want, bound = cache.definition(f64(q), 0.3, dtype)
     assert np.median(bound) < 0.04 * np.sqrt(np.mean(want ** 2))
     check(attend(api, cache, q, 0.3), want, bound)
+
+
+# ------------------------------------------------------------------ offsets and lengths out of range
+def append_ones(api, cu, lens, n_tokens, page):
+    """The status after appending ones to an empty cache."""
+    d, width = 64, -(-max(lens) // page)
+    x = torch.ones(n_tokens, 1, d, dtype=torch.float16, device="cuda")
+    tensors = [torch.zeros(len(lens) * width, 1, page, d, dtype=torch.int8, device="cuda") for _ in range(2)] + [torch.zeros(len(lens) * width, 1, device="cuda") for _ in range(2)]
+    api.pd_kv_append(x, x, *tensors, i32(cu), i32(lens), torch.arange(len(lens) * width, dtype=torch.int32, device="cuda").view(-1, width))
+    return api.pd_device_status(api.attn_workspace())
+
+
+@pytest.mark.parametrize("page", [16, 128])
+def test_append_reports_offsets_that_decrease(api, page):
+    for cu, lens in (([0, 1000, 0, 50], [1000, 10, 50]), ([0, 40, 30, 1000], [40, 10, 970]), ([0, 500, 1000, 999, 1000], [500, 500, 0, 1])):
+        assert append_ones(api, cu, lens, 1000, page) == 8, cu
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("new", [1, 5])
+def test_append_reports_one_bad_pair_among_many(api, new, page):
+    """Single tokens (a warp per sequence) and pieces (a block per page): one sequence reaches to the end, the next one down again."""
+    n, cu = 200, [new * i for i in range(201)]
+    assert append_ones(api, cu, [new] * n, cu[-1], page) == 0
+    for at in (0, 1, 30, 31, 32, 100, 198):
+        bad = list(cu)
+        bad[at + 1] = cu[-1] - (at < 198) if at < 198 else cu[at] - 1
+        lens = [max(b - a, new) for a, b in zip(bad, bad[1:])]
+        assert min(b - a for a, b in zip(bad, bad[1:])) < 0
+        assert append_ones(api, bad, lens, cu[-1], page) == 8, at
