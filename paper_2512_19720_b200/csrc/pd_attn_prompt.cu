@@ -248,25 +248,30 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             // Units in the order of their work, most first, so that the blocks end together: the last queries of every sequence
             // that has as many tiles as the longest, then the tile before those, and so on; all heads of a tile in a row.
             // More than 32 sequences are taken 32 at a time.  A lane knows one sequence; ids only grow, so that the walk over
-            // groups and tiles goes forward only.
+            // groups and tiles goes forward only.  Behind offsets that decrease no sequence is taken: those before have no token
+            // in common, so that the work and its ids stay within what the host has counted for n_tokens.
             const int span = slots.by_head ? kTile : 2 * kTile;                     // queries of a unit
             const int per_tile = slots.by_head ? a.q_heads / 2 : a.q_heads;         // units of a tile
             int g0 = -32, first = 0, len = 0, tiles = 0, level = 0, level_base = 0, group_end = 0;
             uint32_t it = 0, n_diag = 0, phase_q = 3;  // bit s: slot s; the places are free at first
-            bool ok = true;
+            bool ok = true, in_order = true;
             int id = blockIdx.x;
             while (ok) {
                 id = __shfl_sync(0xffffffffu, id, 0);
                 while (id >= group_end && g0 < a.n_seqs) {
                     g0 += 32;
                     tiles = 0;
+                    int end = first = 0;
                     if (g0 + lane < a.n_seqs) {
-                        first = __ldg(a.cu_seqlens + g0 + lane);
-                        const int end = __ldg(a.cu_seqlens + g0 + lane + 1);
-                        len = end - first;
+                        first = __ldg(a.cu_seqlens + g0 + lane), end = __ldg(a.cu_seqlens + g0 + lane + 1);
                         if (first < 0 || end < first || end > a.n_tokens) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(g0 + lane));
-                        else tiles = (len + span - 1) / span;
                     }
+                    const unsigned down = __ballot_sync(0xffffffffu, end < first);
+                    if (in_order && !(down & ((2u << lane) - 1u)) && first >= 0 && end <= a.n_tokens) {
+                        len = end - first;
+                        tiles = (len + span - 1) / span;
+                    }
+                    in_order = in_order && !down;
                     level_base = group_end;
                     group_end += __reduce_add_sync(0xffffffffu, tiles) * per_tile;
                     level = __reduce_max_sync(0xffffffffu, tiles) - 1;

@@ -197,3 +197,23 @@ def test_append_reports_one_bad_pair_among_many(api, new, page):
         lens = [max(b - a, new) for a, b in zip(bad, bad[1:])]
         assert min(b - a for a, b in zip(bad, bad[1:])) < 0
         assert append_ones(api, bad, lens, cu[-1], page) == 8, at
+
+
+@pytest.mark.parametrize("hkv,d", [(2, 64), (4, 128)])
+def test_prompt_takes_no_sequence_behind_offsets_that_decrease(api, hkv, d):
+    """Sequences that have tokens in common could be any amount of work: only those before the offsets go down are computed."""
+    gen = torch.Generator("cuda").manual_seed(23)
+    q, k, v = (torch.randn(400, h, d, generator=gen, device="cuda").half() for h in (4, hkv, hkv))
+    alone = api.pd_attn_prompt(q[:100].contiguous(), k[:100].contiguous(), v[:100].contiguous(), offsets([100]))
+    assert api.pd_device_status(api.attn_workspace()) == 0
+    for cu in ([0, 100, 50, 150], [0, 100] + [20, 400] * 40, [0] * 40 + [100, 90] + list(range(90, 400, 10))):
+        out = torch.full((400, 4, d), 7.0, dtype=torch.float16, device="cuda")
+        api.pd_attn_prompt(q, k, v, i32(cu), out=out)
+        assert api.pd_device_status(api.attn_workspace()) == 8
+        assert torch.equal(out[:100], alone) and bool((out[100:] == 7).all()), cu
+    # out of range without going down: the others are served
+    for cu, keep in (([-5, 0, 100], (0, 100)), ([0, 100, 401, 402], (0, 100))):
+        out = torch.full((400, 4, d), 7.0, dtype=torch.float16, device="cuda")
+        api.pd_attn_prompt(q, k, v, i32(cu), out=out)
+        assert api.pd_device_status(api.attn_workspace()) == 8
+        assert torch.equal(out[:100], alone) and bool((out[100:] == 7).all()), cu
