@@ -410,7 +410,7 @@ pd_status pd_attn_prompt_bf16(const void *q, int64_t q_token_stride, int64_t q_h
  * A page and head with new tokens gets the scale s' = max(s, max |new| / 127) (s = 0 where the page's first token is among
  * the new ones, whatever the page held before), its held codes become round(c * (s * (1/s'))) and the new ones
  * round(x * (1/s')), all in binary32 with rounding to nearest even.  A page whose s' is below 2^-120 gets codes of zero; one
- * with an infinity or a NaN among its values reads as NaN.  No page may belong to two sequences of a call.
+ * with an infinity or a NaN among its values too, and reads as NaN (an infinite or NaN scale times zero).  No page may belong to two sequences of a call.
  */
 pd_status pd_kv_append(const void *k, int64_t k_token_stride, int64_t k_head_stride,
                        const void *v, int64_t v_token_stride, int64_t v_head_stride,

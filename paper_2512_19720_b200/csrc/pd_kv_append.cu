@@ -53,11 +53,12 @@ __device__ __forceinline__ float warp_magnitude(uint32_t most) {
 }
 
 struct Scale {
-    float s, inv;  // 1 / s; 0 where s is too small for it or infinite (a NaN scale gives codes of 0 too)
+    float s, inv;    // 1 / s; 0 where s is too small for it, infinite or NaN
+    uint32_t keep;   // bits of the codes: none where inv is 0, so that an infinite scale times any code of the page is NaN too
 };
 __device__ __forceinline__ Scale scale_of(float s_old, float amax) {
-    const float s = max_nan(s_old, __fdiv_rn(amax, 127.f));
-    return {s, s >= 0x1p-120f ? __frcp_rn(s) : 0.f};
+    const float s = max_nan(s_old, __fdiv_rn(amax, 127.f)), inv = s >= 0x1p-120f ? __frcp_rn(s) : 0.f;
+    return {s, inv, inv > 0.f ? 0xffffffffu : 0u};
 }
 
 // eight values to their codes and, unless nullptr, to the values that those stand for
@@ -71,7 +72,7 @@ __device__ __forceinline__ void store8(const uint4 &raw, const Scale &sc, int8_t
         const float2 t = E::to_float2(w[j]);
         f[2 * j] = __fadd_rn(__fmul_rn(t.x, sc.inv), kShift), f[2 * j + 1] = __fadd_rn(__fmul_rn(t.y, sc.inv), kShift);
     }
-    *reinterpret_cast<uint2 *>(codes) = make_uint2(low_bytes(f[0], f[1], f[2], f[3]), low_bytes(f[4], f[5], f[6], f[7]));
+    *reinterpret_cast<uint2 *>(codes) = make_uint2(low_bytes(f[0], f[1], f[2], f[3]) & sc.keep, low_bytes(f[4], f[5], f[6], f[7]) & sc.keep);
     if (values) {
         uint32_t o[4];
 #pragma unroll
@@ -80,8 +81,9 @@ __device__ __forceinline__ void store8(const uint4 &raw, const Scale &sc, int8_t
     }
 }
 
-// sixteen held codes of the smaller scale to those of the larger one
-__device__ __forceinline__ void scale_again16(uint4 *p, float ratio) {
+// sixteen held codes of the smaller scale s_old to those of the larger one
+__device__ __forceinline__ void scale_again16(uint4 *p, float s_old, const Scale &sc) {
+    const float ratio = s_old * sc.inv;
     const uint4 c = *p;
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
     uint32_t r[4];
@@ -90,7 +92,7 @@ __device__ __forceinline__ void scale_again16(uint4 *p, float ratio) {
         float f[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) f[k] = __fadd_rn(__fmul_rn(static_cast<float>(static_cast<int8_t>(w[j] >> (8 * k))), ratio), kShift);
-        r[j] = low_bytes(f[0], f[1], f[2], f[3]);
+        r[j] = low_bytes(f[0], f[1], f[2], f[3]) & sc.keep;
     }
     *p = make_uint4(r[0], r[1], r[2], r[3]);
 }
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(kMaxThreads, 4) append_pages_kernel(const Appe
     for (int w = 1; w < static_cast<int>(blockDim.x >> 5); ++w) amax = max_nan(amax, red[w]);
     const Scale sc = scale_of(s_old, amax);
     if (held && sc.s != s_old)
-        for (int at = threadIdx.x; at < held * (D / 16); at += blockDim.x) scale_again16(reinterpret_cast<uint4 *>(codes) + at, s_old * sc.inv);
+        for (int at = threadIdx.x; at < held * (D / 16); at += blockDim.x) scale_again16(reinterpret_cast<uint4 *>(codes) + at, s_old, sc);
     int8_t *to = codes + (held + tok) * D + 8 * piece;
     uint16_t *values = static_cast<uint16_t *>(a.values[which]);
     if (values) values += (tok0 * a.kv_heads + head) * D + 8 * piece;
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(kTokenWarps * 32) append_tokens_kernel(const A
         for (int tok = mine + kSide; tok < n; tok += kSide) most = magnitude2(load(tok), most);
         const Scale sc = scale_of(s_old, warp_magnitude<BF16>(most));
         if (held && sc.s != s_old)
-            for (int at = lane; at < held * (D / 16); at += 32) scale_again16(reinterpret_cast<uint4 *>(codes) + at, s_old * sc.inv);
+            for (int at = lane; at < held * (D / 16); at += 32) scale_again16(reinterpret_cast<uint4 *>(codes) + at, s_old, sc);
         for (int tok = mine; tok < n; tok += kSide) {
             // in-place values: a token is read for the last time by the lane that then writes it
             const uint4 v = tok == mine ? raw : *reinterpret_cast<const uint4 *>(x + (tok0 + tok) * a.x[which].token_stride);

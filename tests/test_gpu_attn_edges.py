@@ -217,3 +217,36 @@ def test_prompt_takes_no_sequence_behind_offsets_that_decrease(api, hkv, d):
         api.pd_attn_prompt(q, k, v, i32(cu), out=out)
         assert api.pd_device_status(api.attn_workspace()) == 8
         assert torch.equal(out[:100], alone) and bool((out[100:] == 7).all()), cu
+
+
+# ------------------------------------------------------------------ infinities and NaN among the keys
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("at", [64, 70, 20])
+def test_a_key_that_is_not_finite_reads_as_nan(api, at, bad, dtype):
+    """Alone in its page, among others, appended in one call or by itself, whatever the sign of the query: NaN, and codes of zero."""
+    d, page, n = 64, 32, at + 1 if at > 32 else 65
+    gen = torch.Generator("cuda").manual_seed(29)
+    k, v = (torch.randn(n, 2, d, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    k[at, 1, 9] = bad
+    q = torch.randn(1, 4, d, generator=gen, device="cuda").to(dtype)
+    table = i32([[2, 0, 1]])
+    for steps in ([n], [at, n - at], [at] + [1] * (n - at)):
+        tensors = [torch.full((3, 2, page, d), 55, dtype=torch.int8, device="cuda") for _ in range(2)] + [torch.zeros(3, 2, device="cuda") for _ in range(2)]
+        held = 0
+        for m in steps:
+            values = torch.empty(m, 2, d, dtype=dtype, device="cuda")
+            api.pd_kv_append(k[held:held + m].contiguous(), v[held:held + m].contiguous(), *tensors, offsets([m]), i32([held + m]), table, values)
+            held += m
+        p = [2, 0, 1][at // page]
+        assert not tensors[0][p, 1, :min(page, n - at // page * page)].any()
+        scale = float(tensors[2][p, 1])
+        assert scale != scale if bad != bad else scale == float("inf")
+        if at // page == (n - 1) // page:  # the values of the last call's tokens in that page
+            assert bool(torch.isnan(values[max(at // page * page - (n - m), 0):, 1]).all())
+        for sign in (1, -1):
+            query = q.clone()
+            query[:, 2:, 9] = sign * 2.0
+            got = api.pd_attn_cache(query, *tensors, i32([n]), table)
+            assert bool(torch.isnan(got[:, 2:]).all()) and bool(torch.isfinite(got[:, :2]).all())
+    assert api.pd_device_status(api.attn_workspace()) == 0
