@@ -509,8 +509,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const uint32_t ts = lanes + kColS, tp = lanes + kColP + s * 64, to = lanes + kColO + s * 128;
         // The maximum is taken before the scores are scaled, so that the factor is positive: the products give -Q K^T for a
-        // negative scale, and a scale of zero is one that makes nothing of any finite score (minus infinity stays what it is).
-        const float f = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1e-30f;
+        // negative scale, and a scale of zero is one that makes nothing of any finite score (minus infinity stays what it is):
+        // 2^128 * 2^-149 is the most that is left of one.
+        const float f = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 0x1p-149f;
         uint32_t n_s = 0, n_sum = 0;  // tiles and units of the slot so far
         bool ok = true;
         Unit u;

@@ -250,3 +250,17 @@ def test_a_key_that_is_not_finite_reads_as_nan(api, at, bad, dtype):
             got = api.pd_attn_cache(query, *tensors, i32([n]), table)
             assert bool(torch.isnan(got[:, 2:]).all()) and bool(torch.isfinite(got[:, :2]).all())
     assert api.pd_device_status(api.attn_workspace()) == 0
+
+
+# ------------------------------------------------------------------ scales of scores
+@pytest.mark.parametrize("hkv,d", [(2, 64), (4, 128)])
+def test_prompt_with_a_scale_of_zero_and_large_scores(api, hkv, d):
+    """Scores up to 1e37 times zero are zero: means of the values so far.  exp2(2^-21) is off by 2^-21 and is covered by 2^-20 of the mean magnitude."""
+    lens = [150, 290]
+    gen = torch.Generator("cuda").manual_seed(31)
+    q, k, v = (torch.randn(sum(lens), h, d, generator=gen, device="cuda").bfloat16() for h in (4, hkv, hkv))
+    got = f64(api.pd_attn_prompt(q * 2.0 ** 58, k * 2.0 ** 58, v, offsets(lens), 0.0))
+    zero, vd = np.zeros_like(f64(q)), f64(v)
+    want = orc.attn_prompt(zero, np.zeros_like(vd), vd, lens, 0.0)
+    near = orc.attn_prompt(zero, np.zeros_like(vd), np.abs(vd), lens, 0.0)
+    assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -20) * near)
