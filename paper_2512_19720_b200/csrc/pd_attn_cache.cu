@@ -335,13 +335,21 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         }
 
         if (len > 0) {
-            for (int i = i0; i < i1; ++i) {
-                cp_async_wait<kStages - 2>();
-                __syncwarp();
-                issue(i + kStages - 1);
+            // The two 16-token halves of a tile share r: where they are pages whose scales are more than 8 apart, the tile is gone
+            // through twice, once for each half.
+            int half = 0;  // 0: both at once, 1 and 2: one of them
+            for (int i = i0; i < i1; half == 1 ? ++half : (half = 0, ++i)) {
+                if (half < 2) {
+                    cp_async_wait<kStages - 2>();
+                    __syncwarp();
+                    issue(i + kStages - 1);
+                }
                 const int st = (i - i0) % kStages;
                 const unsigned char *ks = ring + st * L::kStage, *vs = ks + kTile * D;
                 const float4 sc = meta[st];
+                if (half == 0 && fmaxf(sc.z, sc.w) > 8.f * fminf(sc.z, sc.w) && fminf(sc.z, sc.w) > 0.f) half = 1;
+                const int rest = static_cast<int>(min(len - static_cast<int64_t>(i) * kTile, static_cast<int64_t>(kTile)));  // tokens of the tile
+                const int end[2] = {half == 2 ? 0 : rest, half == 1 ? 0 : rest};
 
                 // S^T = K Q^T
                 float acc[2][NT][4];
@@ -377,7 +385,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                             acc[h][n][k] = fmaf(f[2], 65536.f, fmaf(f[1], 256.f, f[0]));
                         }
                 }
-                // scores in base 2; places past the end of the sequence are chosen away, whatever they hold
+                // scores in base 2; places past the end of the sequence or of the other half are chosen away, whatever they hold
                 bool lead = false;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -386,11 +394,10 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const float f = (h == 0 ? sc.x : sc.y) * qs[n][k & 1];
-                            const int64_t tok = static_cast<int64_t>(i) * kTile + 16 * h + g + 8 * (k >> 1);
-                            acc[h][n][k] = tok < len ? acc[h][n][k] * f : -INFINITY;
+                            acc[h][n][k] = 16 * h + g + 8 * (k >> 1) < end[h] ? acc[h][n][k] * f : -INFINITY;
                             lead |= acc[h][n][k] > m[n][k & 1] + kMaxLead;
                         }
-                const float sv_hi = fmaxf(sc.z, sc.w);
+                const float sv[2] = {half == 2 ? 0.f : sc.z, half == 1 ? 0.f : sc.w}, sv_hi = fmaxf(sv[0], sv[1]);
                 const bool move_ref = sv_hi > 8.f * ref || (sv_hi < 0.125f * ref && sv_hi > 0.f);
                 if (__any_sync(0xffffffffu, lead) || move_ref) {
                     float factor[NT][2];  // for O
@@ -438,7 +445,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
 #pragma unroll
                             for (int k = 0; k < 4; ++k) o[j][n][k] *= factor[n][k & 1];
                 }
-                const float rv[2] = {sc.z == 0.f ? 0.f : sc.z * inv_ref, sc.w == 0.f ? 0.f : sc.w * inv_ref};
+                const float rv[2] = {sv[0] * inv_ref, sv[1] * inv_ref};
                 uint32_t pf[2][NT][2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)

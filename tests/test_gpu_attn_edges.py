@@ -2,8 +2,9 @@
 
 Bound of pd_attn_cache, for each output, with w_j the weights and M the largest score of the row, L = sum_j e^(s_j - M):
   - rounding to the output's type: u_out |out| (u = 2^-11 for binary16, 2^-8 for bfloat16), and its smallest step;
-  - P in binary16: 2^-11 sum_j w_j |v_j|; where P is subnormal 2^-25 of a unit, which is at most 8 page scales of the tile and at
-    most 1 / L of a weight: 2^-22 / L sum_j (largest page scale of j's tile) |code_j|;
+  - P in binary16: 2^-11 sum_j w_j |v_j|; where P is subnormal 2^-25 of a unit, which is at most 64 page scales (the reference
+    scale is at most 8 times a tile's largest, that at most 8 times the other one of the tile) and at most 1 / L of a weight,
+    and never more than the weight itself: sum_j min(w_j, 2^-19 / L) |v_j|; where V's scales are 2^100 apart, what is far below does not count: 2^-90 of the largest |v_j|;
   - scores: a query is a multiple of 2^-21 of the power of two below its largest value, so that a score is off by
     d_j <= scale 2^-22 max|q| sum |k_j|; binary32 arithmetic adds 2^-20 (|s_j| + 1).  Weights are off by e^(2 max d) - 1 then."""
 import numpy as np
@@ -73,13 +74,11 @@ class Cache:
                 e = np.exp(s - s.max())
                 w = e / e.sum()
                 v = vc * sv[:, None]
-                tile = np.arange(len(s)) // 32
-                tile_scale = np.maximum.reduceat(sv, np.arange(0, len(s), 32))[tile]
                 off = (abs(scale) * 2.0 ** -22 * np.abs(q[b, h]).max() * np.abs(kc).sum(1) * sk + 2.0 ** -20 * (np.abs(s) + 1)).max()
                 near = w @ np.abs(v)
                 out[b, h] = w @ v
                 bound[b, h] = (UNIT[dtype] * np.abs(out[b, h]) + SMALLEST[dtype] + (2.0 ** -11 + np.expm1(2 * off)) * near +
-                               2.0 ** -22 / e.sum() * (tile_scale @ np.abs(vc)))
+                               np.minimum(w, 2.0 ** -19 / e.sum()) @ np.abs(v) + 2.0 ** -90 * np.abs(v).max())
         return out, bound
 
 
@@ -110,6 +109,25 @@ def test_cache_values_with_scales_of_any_size(api, hq, hkv, d, page):
     want, bound = cache.definition(f64(q), d ** -0.5, torch.bfloat16)
     check(attend(api, cache, q, d ** -0.5), want, bound)
     assert not want[0].any() and np.median(bound[1:5] / np.abs(want[1:5])) < 0.05
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (12, 1, 64), (32, 2, 128)])
+def test_cache_pages_of_a_tile_with_very_different_scales(api, hq, hkv, d, dtype):
+    """Pages of 16 tokens, every other one with values far above the rest and with keys that hardly any head attends to: what the
+    heads do attend to is not rounded by the neighbours' scale."""
+    lens = [16 * 9 + 5, 16 * 40, 31]
+    apart = {torch.float16: (2.0 ** 14, 2.0 ** -10), torch.bfloat16: (2.0 ** 30, 2.0 ** -30)}[dtype]
+    for odd in (0, 1):
+        cache = Cache(lens, hkv, d, 16, 37)
+        large = (np.arange(len(cache.k_codes)) + odd) % 2 == 0
+        cache.v_scale[large], cache.v_scale[~large] = np.float32(apart[0] / 127), np.float32(apart[1])
+        cache.k_codes[large, :, :, 0], cache.k_codes[~large, :, :, 0] = -127, 0
+        q = torch.randn(len(lens), hq, d, generator=torch.Generator("cuda").manual_seed(41), device="cuda").to(dtype)
+        q[..., 0] = 800.0
+        want, bound = cache.definition(f64(q), d ** -0.5, dtype)
+        assert np.abs(want[1]).max() < 2.0 ** 8 * apart[1] and np.median(bound[1]) < 0.1 * np.sqrt(np.mean(want[1] ** 2))
+        check(attend(api, cache, q, d ** -0.5), want, bound)
 
 
 def test_appended_values_that_are_tiny(api):
