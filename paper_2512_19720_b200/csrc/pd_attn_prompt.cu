@@ -3,7 +3,9 @@
 // One pass over the keys with a running maximum m and sum l of each query row (32 bits, base 2): with s the scores of a tile,
 //     m' = max(m, max s),  l' = l 2^(m - m') + sum 2^(s - m'),  O' = O 2^(m - m') + 2^(s - m') V,  out = O / l at the end.
 // P = 2^(s - m') is rounded to the type of v for its product; l sums the unrounded values.  m only moves when a score passes
-// it by more than 8, so that O is hardly ever rescaled: P is then at most 2^8 and its relative rounding is the same.
+// it by more than 8, so that O is hardly ever rescaled: P is then at most 2^8 and its relative rounding is the same.  In
+// binary16 P and l are 2^7 times that, which is what its range has room for: weights down to 2^-21 of the largest keep their
+// precision, those below lose up to 2^-32 of it.
 //
 // Bound by the tensor cores (4 * head_dim operations per query, key and head) and, as nearly, by the exponentials: a tile of
 // 128 x 128 scores is 1024 clocks of products at head_dim 128 and 1024 clocks of the 16 exponentials a clock that an SM has.
@@ -40,6 +42,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kUnits = 4;  // units that the producer may be ahead
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLead = 8.f;  // how far (base-2 exponent) a score may pass the reference maximum
+constexpr float kRoom = 7.f;     // the exponent by which P is larger than the weights in binary16
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;  // tensor-memory columns; slot 1: P + 64, O + 128
 
 struct Unit {
@@ -565,9 +568,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 };
                 if (__any_sync(0xffffffffu, best > m + kMaxLead)) {
                     if (!(ok = until_done())) break;
-                    const float now = fmaxf(m, best), mu_new = now == -INFINITY ? 0.f : now;
-                    const float shrink = exp2_approx(m - mu_new);  // 0 from -infinity on
-                    m = now, mu = mu_new;
+                    const float now = fmaxf(m, best), base = now == -INFINITY ? 0.f : now;
+                    const float shrink = exp2_approx(m - base);  // 0 from -infinity on
+                    m = now, mu = BF16 ? base : base - kRoom;
                     l.x *= shrink, l.y *= shrink;
                     if (j > 0) {
 #pragma unroll 1

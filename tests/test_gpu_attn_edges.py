@@ -282,3 +282,21 @@ def test_prompt_with_a_scale_of_zero_and_large_scores(api, hkv, d):
     want = orc.attn_prompt(zero, np.zeros_like(vd), vd, lens, 0.0)
     near = orc.attn_prompt(zero, np.zeros_like(vd), np.abs(vd), lens, 0.0)
     assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -20) * near)
+
+
+@pytest.mark.parametrize("hkv,d", [(2, 64), (4, 128)])
+@pytest.mark.parametrize("gap", [16.6, 20.6, 23.42, 25.2])
+def test_prompt_many_small_weights_beside_a_large_one(api, hkv, d, gap):
+    """A prompt in binary16 whose first token holds nearly all of the weight, the others the rest, which is what the outputs are made
+    of.  Each of them loses at most 2^-32 of the first one's weight."""
+    n = 6000
+    q, k = torch.zeros(n, 4, d, dtype=torch.float16, device="cuda"), torch.zeros(n, hkv, d, dtype=torch.float16, device="cuda")
+    v = torch.rand(n, hkv, d, generator=torch.Generator("cuda").manual_seed(47), device="cuda").half() + 1000
+    q[..., 3], k[0, :, 3], v[0] = 1.0, 1.0, 0.0
+    scale = float(np.float32(gap * np.log(2)))
+    got = f64(api.pd_attn_prompt(q, k, v, offsets([n]), scale))
+    vd = np.repeat(f64(v), 4 // hkv, axis=1)
+    w = np.exp(-scale) / (1 + np.exp(-scale) * np.arange(n))[:, None, None]  # of each token but the first
+    want = w * np.cumsum(vd, axis=0)
+    assert np.all(np.abs(got - want)[1:] <= ((2 * 2.0 ** -11 + 2.0 ** -14) * want + 2.0 ** -24 + 2.0 ** -32 * np.arange(n)[:, None, None] * 1001)[1:])
+    assert 2.0 ** -32 < 0.01 * np.exp(-scale)
