@@ -69,17 +69,27 @@ class Cache:
         group = q.shape[1] // self.k_codes.shape[1]
         for b in range(len(self.lens)):
             for h in range(q.shape[1] if self.lens[b] else 0):
-                kc, vc, sk, sv = self.rows(b, h // group)
+                if h % group == 0:
+                    kc, vc, sk, sv = self.rows(b, h // group)
+                    v, magnitude = vc * sv[:, None], np.abs(vc) * sv[:, None]
+                    k_sum = np.abs(kc).sum(1) * sk
                 s = (kc @ q[b, h]) * sk * scale
                 e = np.exp(s - s.max())
                 w = e / e.sum()
-                v = vc * sv[:, None]
-                off = (abs(scale) * 2.0 ** -22 * np.abs(q[b, h]).max() * np.abs(kc).sum(1) * sk + 2.0 ** -20 * (np.abs(s) + 1)).max()
-                near = w @ np.abs(v)
+                off = (abs(scale) * 2.0 ** -22 * np.abs(q[b, h]).max() * k_sum + 2.0 ** -20 * (np.abs(s) + 1)).max()
+                near = w @ magnitude
                 out[b, h] = w @ v
                 bound[b, h] = (UNIT[dtype] * np.abs(out[b, h]) + SMALLEST[dtype] + (2.0 ** -11 + np.expm1(2 * off)) * near +
-                               np.minimum(w, 2.0 ** -19 / e.sum()) @ np.abs(v) + 2.0 ** -90 * np.abs(v).max())
+                               np.minimum(w, 2.0 ** -19 / e.sum()) @ magnitude + 2.0 ** -90 * magnitude.max())
         return out, bound
+
+    def without(self, q, scale, b, h):
+        """Row (b, h) with each of its 32-token tiles left out: [tiles, d]."""
+        kc, vc, sk, sv = self.rows(b, h * self.k_codes.shape[1] // q.shape[1])
+        s = (kc @ q[b, h]) * sk * scale
+        e, at = np.exp(s - s.max()), np.arange(0, len(s), 32)
+        total, value = np.add.reduceat(e, at), np.add.reduceat((e * sv)[:, None] * vc, at)
+        return (value.sum(0) - value) / (total.sum() - total)[:, None]
 
 
 def check(got, want, bound):
@@ -300,3 +310,29 @@ def test_prompt_many_small_weights_beside_a_large_one(api, hkv, d, gap):
     want = w * np.cumsum(vd, axis=0)
     assert np.all(np.abs(got - want)[1:] <= ((2 * 2.0 ** -11 + 2.0 ** -14) * want + 2.0 ** -24 + 2.0 ** -32 * np.arange(n)[:, None, None] * 1001)[1:])
     assert 2.0 ** -32 < 0.01 * np.exp(-scale)
+
+
+# ------------------------------------------------------------------ long sequences, cut into parts
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens", [[333], [7, 9000], [20011], [640] * 40], ids=["333", "7, 9000", "20011", "40 x 640"])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 128), (16, 2, 64), (32, 2, 128), (40, 1, 128), (1, 1, 64)])
+def test_cache_every_tile_counts(api, hq, hkv, d, lens, dtype):
+    """The work of a sequence is cut into parts that are joined.  A tile's values are in one dimension of the output, which it shares
+    with few others, so that the bound would catch any tile that is lost or counted twice: checked of the definition here."""
+    cache = Cache(lens, hkv, d, 64, 53)
+    tile = np.arange(cache.table.shape[1] * 64).reshape(-1, 64) // 32
+    for b in range(len(lens)):
+        n = -(-lens[b] // 64)
+        one = (np.arange(d) == tile[:n, :, None] % d)[:, None]
+        cache.v_codes[cache.table[b, :n]] = one * (64 + np.abs(cache.v_codes[cache.table[b, :n]].astype(np.int64)) // 2)
+    q = torch.randn(len(lens), hq, d, generator=torch.Generator("cuda").manual_seed(59), device="cuda").to(dtype)
+    want, bound = cache.definition(f64(q), 0.02, dtype)
+    assert np.median(bound[want > 0] / want[want > 0]) < 2.5 * (UNIT[dtype] + 2.0 ** -11)
+    for b in {0, len(lens) - 1}:
+        for h in {0, hq - 1}:
+            assert (want[b, h] > 2 * bound[b, h]).any()
+            if lens[b] > 32:
+                assert np.all((np.abs(cache.without(f64(q), 0.02, b, h) - want[b, h]) > 2 * bound[b, h]).any(axis=1))
+    got = attend(api, cache, q, 0.02)
+    check(got, want, bound)
+    assert torch.equal(got, attend(api, cache, q, 0.02))
