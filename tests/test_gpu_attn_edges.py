@@ -336,3 +336,38 @@ def test_cache_every_tile_counts(api, hq, hkv, d, lens, dtype):
     got = attend(api, cache, q, 0.02)
     check(got, want, bound)
     assert torch.equal(got, attend(api, cache, q, 0.02))
+
+
+# ------------------------------------------------------------------ forms of calls that a server makes
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new", [[1] * 63 + [190], [190] + [1] * 63, [1, 0, 0, 77, 1, 1, 0, 1] * 5, [0] * 30 + [100] + [0] * 9], ids=["end", "start", "some", "one"])
+def test_append_of_single_tokens_with_longer_pieces(api, new, dtype):
+    """Decode tokens and a piece of a prompt in one call: the same bits as each sequence by itself."""
+    hkv, d, page = 2, 128, 32
+    held = [(37 * b) % 100 for b in range(len(new))]
+    total = [a + b for a, b in zip(held, new)]
+    width = max(total) // page + 1
+    gen = torch.Generator("cuda").manual_seed(61)
+    kv = torch.randn(sum(new), 2 * hkv, d, generator=gen, device="cuda").to(dtype)
+    wide = torch.arange(len(new) * (width + 3), dtype=torch.int32, device="cuda").view(len(new), width + 3).flip(0)
+    table = wide[:, :width]  # rows further apart than they are wide
+    codes = torch.randint(-127, 128, (wide.numel(), hkv, page, d), generator=gen, device="cuda", dtype=torch.int8)
+    scale = torch.rand(wide.numel(), hkv, generator=gen, device="cuda") * 0.03
+
+    def fresh():
+        return [codes.clone(), codes.flip(0).contiguous(), scale.clone(), scale.flip(0).contiguous()]
+    together, single = fresh(), fresh()
+    values = [torch.empty(sum(new), hkv, d, dtype=dtype, device="cuda") for _ in range(2)]
+    api.pd_kv_append(kv[:, :hkv], kv[:, hkv:], *together, offsets(new), i32(total), table, *values)
+    at = 0
+    for b, m in enumerate(new):
+        if m:
+            x = kv[at:at + m]
+            out = [torch.empty(m, hkv, d, dtype=dtype, device="cuda") for _ in range(2)]
+            api.pd_kv_append(x[:, :hkv], x[:, hkv:], *single, offsets([m]), i32(total[b:b + 1]), table[b:b + 1].contiguous(), *out)
+            assert torch.equal(values[0][at:at + m], out[0]) and torch.equal(values[1][at:at + m], out[1])
+            at += m
+    assert api.pd_device_status(api.attn_workspace()) == 0
+    assert all(torch.equal(x, y) for x, y in zip(together, single))
+    q = torch.randn(len(new), 4, d, generator=gen, device="cuda").to(dtype)
+    assert torch.equal(api.pd_attn_cache(q, *together, i32(total), table), api.pd_attn_cache(q, *together, i32(total), table.contiguous()))
