@@ -42,6 +42,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kUnits = 4;  // units that the producer may be ahead
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLead = 8.f;  // how far (base-2 exponent) a score may pass the reference maximum
+constexpr float kFar = 1024.f;   // reference maxima (base-2 exponent) from which on scores are taken from them before they are scaled
 constexpr float kRoom = 7.f;     // the exponent by which P is larger than the weights in binary16
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;  // tensor-memory columns; slot 1: P + 64, O + 128
 
@@ -524,7 +525,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 done_unit();
                 continue;
             }
-            float m = -INFINITY, mu = 0.f;
+            float m = -INFINITY;  // of the scores before they are scaled
+            float sub1 = 0.f;     // what the exponents get added: -m f, and the room of P
+            bool far = false;     // the same in all lanes
             float2 l = make_float2(0.f, 0.f);
             for (int j = 0; j < n; ++j, ++n_s) {
                 if (!(ok = wait_warp(bar.s_full + s, n_s, 60))) break;
@@ -556,7 +559,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                     for (int k = 1; k < 31; k += 2) top[c] = max3(top[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
                 }
-                const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * f;
+                const float best = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 // Before O is rescaled or P written the product with the tile before has to be done.
                 bool may_write = n_s == 0;
                 auto until_done = [&]() {
@@ -566,11 +569,15 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                     return may_write;
                 };
-                if (__any_sync(0xffffffffu, best > m + kMaxLead)) {
+                if (__any_sync(0xffffffffu, best * f > fmaf(m, f, kMaxLead))) {
                     if (!(ok = until_done())) break;
                     const float now = fmaxf(m, best), base = now == -INFINITY ? 0.f : now;
-                    const float shrink = exp2_approx(m - base);  // 0 from -infinity on
-                    m = now, mu = BF16 ? base : base - kRoom;
+                    const float shrink = exp2_approx((m - base) * f);  // 0 from -infinity on
+                    m = now;
+                    // x f - m f in one step keeps the rounding of m f: half a unit in its last place, which would be most of P's
+                    // range, and more, for large scores.
+                    far = __any_sync(0xffffffffu, fabsf(base * f) >= kFar) != 0;
+                    sub1 = (far ? 0.f : -base * f) + (BF16 ? 0.f : kRoom);
                     l.x *= shrink, l.y *= shrink;
                     if (j > 0) {
 #pragma unroll 1
@@ -585,7 +592,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         tcgen05_wait_st();
                     }
                 }
-                const float2 ff = make_float2(f, f), sub = make_float2(-mu, -mu);
+                if (far) {
+                    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[c][k] = __float_as_uint(__uint_as_float(x[c][k]) - base);
+                }
+                const float2 ff = make_float2(f, f), sub = make_float2(sub1, sub1);
                 auto quarter = [&](const uint32_t (&w)[32], uint32_t *p) {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {

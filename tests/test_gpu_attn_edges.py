@@ -294,6 +294,40 @@ def test_prompt_with_a_scale_of_zero_and_large_scores(api, hkv, d):
     assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -20) * near)
 
 
+@pytest.mark.parametrize("dtype,sizes", [(torch.float16, (300.0, 3000.0, 15000.0)), (torch.bfloat16, (300.0, 1e5, 1e9, 1e14))], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (3, 3, 128)])
+def test_prompt_with_scores_of_any_size(api, hq, hkv, d, dtype, sizes):
+    """Finite scores give finite outputs, however large: nearly always all of the weight is one token's.  A score is off by at most
+    2^-18 sum_d |q_d k_d| of the sums and products in binary32, and weights by e^(twice that)."""
+    lens = [300, 77]
+    gen = torch.Generator("cuda").manual_seed(67)
+    q, k, v = (torch.randn(sum(lens), h, d, generator=gen, device="cuda") for h in (hq, hkv, hkv))
+    for size in sizes:
+        most = 6e4 if dtype == torch.float16 else 3e38  # so that they are finite
+        qs, ks, vs = (q * size).clamp(-most, most).to(dtype), (k * size).clamp(-most, most).to(dtype), v.to(dtype)
+        for scale in (d ** -0.5, -0.3):
+            got = f64(api.pd_attn_prompt(qs, ks, vs, offsets(lens), scale))
+            assert np.all(np.isfinite(got))
+            want, near, sure = np.zeros_like(got), np.zeros_like(got), np.zeros(got.shape[:2], bool)
+            qd, kd, vd, at = f64(qs), np.repeat(f64(ks), hq // hkv, axis=1), np.repeat(f64(vs), hq // hkv, axis=1), 0
+            for n in lens:
+                for h in range(hq):
+                    s = qd[at:at + n, h] @ kd[at:at + n, h].T * scale
+                    off = np.abs(qd[at:at + n, h]) @ np.abs(kd[at:at + n, h]).T * abs(scale) * 2.0 ** -18
+                    s = np.where(np.tri(n, dtype=bool), s, -np.inf)
+                    w = np.exp(s - s.max(axis=1, keepdims=True))
+                    w /= w.sum(axis=1, keepdims=True)
+                    want[at:at + n, h], near[at:at + n, h] = w @ vd[at:at + n, h], w @ np.abs(vd[at:at + n, h])
+                    # rows where the largest score is larger than the others by more than what both may be off, and 30
+                    low = np.where(np.tri(n, dtype=bool), s + off, -np.inf)
+                    best = s.argmax(axis=1)
+                    low[np.arange(n), best] = -np.inf
+                    sure[at:at + n, h] = s.max(axis=1) - off[np.arange(n), best] > low.max(axis=1) + 30
+                at += n
+            assert sure.mean() > 0.9
+            assert np.all(np.abs(got - want)[sure] <= (UNIT[dtype] * np.abs(want) + (UNIT[dtype] + 2.0 ** -14) * near)[sure])
+
+
 @pytest.mark.parametrize("hkv,d", [(2, 64), (4, 128)])
 @pytest.mark.parametrize("gap", [16.6, 20.6, 23.42, 25.2])
 def test_prompt_many_small_weights_beside_a_large_one(api, hkv, d, gap):
