@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                         for (int k = 0; k < 4; ++k) {
                             const float f = (h == 0 ? sc.x : sc.y) * qs[n][k & 1];
                             acc[h][n][k] = 16 * h + g + 8 * (k >> 1) < end[h] ? acc[h][n][k] * f : -INFINITY;
-                            lead |= acc[h][n][k] > m[n][k & 1] + kMaxLead;
+                            lead |= acc[h][n][k] > __fadd_rd(m[n][k & 1], kMaxLead);  // rounded down: P's range is bounded for large scores too
                         }
                 const float sv[2] = {half == 2 ? 0.f : sc.z, half == 1 ? 0.f : sc.w}, sv_hi = fmaxf(sv[0], sv[1]);
                 const bool move_ref = sv_hi > 8.f * ref || (sv_hi < 0.125f * ref && sv_hi > 0.f);

@@ -569,7 +569,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                     return may_write;
                 };
-                if (__any_sync(0xffffffffu, best * f > fmaf(m, f, kMaxLead))) {
+                if (__any_sync(0xffffffffu, (best - m) * f > kMaxLead)) {
                     if (!(ok = until_done())) break;
                     const float now = fmaxf(m, best), base = now == -INFINITY ? 0.f : now;
                     const float shrink = exp2_approx((m - base) * f);  // 0 from -infinity on

@@ -328,6 +328,34 @@ def test_prompt_with_scores_of_any_size(api, hq, hkv, d, dtype, sizes):
             assert np.all(np.abs(got - want)[sure] <= (UNIT[dtype] * np.abs(want) + (UNIT[dtype] + 2.0 ** -14) * near)[sure])
 
 
+def test_cache_scores_whose_spacing_passes_the_lead(api):
+    """Scores near 2^27 (base 2), 16 apart in binary32: a tile that leads by one step moves the reference maximum, whatever that rounds to.
+    Every sequence is whole in one warp, which goes through its two tiles in turn."""
+    d, n_seqs, hkv = 64, 96, 32
+    cache = Cache([64] * n_seqs, hkv, d, 32, 71)
+    cache.k_codes[:], cache.k_scale[:], cache.v_scale[:] = 0, 1.0, 1.0
+    cache.k_codes[..., 0] = 127
+    for b in range(n_seqs):
+        cache.k_codes[cache.table[b, 0], ..., 1], cache.k_codes[cache.table[b, 1], ..., 1] = b, b + 1
+    cache.v_codes[0::2], cache.v_codes[1::2] = 1, -1
+    q = torch.zeros(n_seqs, hkv, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0], q[..., 1] = 750000.0, 11.0
+    got = f64(attend(api, cache, q, 1.0))
+    assert np.all(np.abs(got) <= 1)
+
+
+def test_prompt_scores_whose_spacing_passes_the_lead(api):
+    """The same of prompts in binary16: each tile of 128 keys leads the one before by 8 in a score near 2^26.5."""
+    n, d = 1280, 64
+    for start in range(0, 64, 8):
+        q, k, v = (torch.zeros(n, 2, d, dtype=torch.float16, device="cuda") for _ in range(3))
+        q[..., 0], k[..., 0], q[..., 1] = 30000.0, 3130.0, 1.0
+        k[..., 1] = (start + 8 * (torch.arange(n, device="cuda") // 128))[:, None].half()
+        v[:] = torch.where(torch.arange(n, device="cuda") // 128 % 2 == 0, 1.0, -1.0)[:, None, None].half()
+        got = f64(api.pd_attn_prompt(q, k, v, offsets([n]), 1.0))
+        assert np.all(np.abs(got) <= 1)
+
+
 @pytest.mark.parametrize("hkv,d", [(2, 64), (4, 128)])
 @pytest.mark.parametrize("gap", [16.6, 20.6, 23.42, 25.2])
 def test_prompt_many_small_weights_beside_a_large_one(api, hkv, d, gap):
