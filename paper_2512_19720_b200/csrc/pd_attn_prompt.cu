@@ -5,7 +5,8 @@
 // P = 2^(s - m') is rounded to the type of v for its product; l sums the unrounded values.  m only moves when a score passes
 // it by more than 8, so that O is hardly ever rescaled: P is then at most 2^8 and its relative rounding is the same.  In
 // binary16 P and l are 2^7 times that, which is what its range has room for: weights down to 2^-21 of the largest keep their
-// precision, those below lose up to 2^-32 of it.
+// precision, those below lose up to 2^-32 of it.  In bfloat16 they are 2^-24 times that, so that O, which is divided by l at the
+// end, stays in range beside values of any size.
 //
 // Bound by the tensor cores (4 * head_dim operations per query, key and head) and, as nearly, by the exponentials: a tile of
 // 128 x 128 scores is 1024 clocks of products at head_dim 128 and 1024 clocks of the 16 exponentials a clock that an SM has.
@@ -43,7 +44,7 @@ constexpr int kUnits = 4;  // units that the producer may be ahead
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLead = 8.f;  // how far (base-2 exponent) a score may pass the reference maximum
 constexpr float kFar = 1024.f;   // reference maxima (base-2 exponent) from which on scores are taken from them before they are scaled
-constexpr float kRoom = 7.f;     // the exponent by which P is larger than the weights in binary16
+constexpr float kRoom = 7.f, kRoomBf16 = -24.f;  // the exponent by which P is larger than the weights in binary16 and bfloat16
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;  // tensor-memory columns; slot 1: P + 64, O + 128
 
 struct Unit {
@@ -577,7 +578,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     // x f - m f in one step keeps the rounding of m f: half a unit in its last place, which would be most of P's
                     // range, and more, for large scores.
                     far = __any_sync(0xffffffffu, fabsf(base * f) >= kFar) != 0;
-                    sub1 = (far ? 0.f : -base * f) + (BF16 ? 0.f : kRoom);
+                    sub1 = (far ? 0.f : -base * f) + (BF16 ? kRoomBf16 : kRoom);
                     l.x *= shrink, l.y *= shrink;
                     if (j > 0) {
 #pragma unroll 1

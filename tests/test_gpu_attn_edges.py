@@ -357,6 +357,27 @@ def test_prompt_scores_whose_spacing_passes_the_lead(api):
 
 
 @pytest.mark.parametrize("hkv,d", [(2, 64), (4, 128)])
+@pytest.mark.parametrize("exponent", [127, 100, -90])
+def test_prompt_values_at_the_ends_of_bfloat16(api, hkv, d, exponent):
+    """Means of finite values are finite, up to the largest that bfloat16 has, and small ones keep their precision."""
+    lens = [1500, 90]
+    gen = torch.Generator("cuda").manual_seed(73)
+    q, k, v = (torch.randn(sum(lens), h, d, generator=gen, device="cuda") for h in (4, hkv, hkv))
+    q, k, v = q.bfloat16(), k.bfloat16(), ((v * 0.3).clamp(-1, 1) * 1.9921875 * 2.0 ** exponent).bfloat16()
+    assert bool(torch.isfinite(v).all())
+    got, vd = f64(api.pd_attn_prompt(q, k, v, offsets(lens))), f64(v)
+    rows = list(range(0, 1500, 50)) + [1499, 1500, 1501, 1589]
+    for i in rows:
+        first = 0 if i < 1500 else 1500
+        for h in range(4):
+            s = f64(k[first:i + 1, h * hkv // 4]) @ f64(q[i, h]) * d ** -0.5
+            w = np.exp(s - s.max())
+            w /= w.sum()
+            x = vd[first:i + 1, h * hkv // 4]
+            assert np.all(np.abs(got[i, h] - w @ x) <= 2.0 ** -8 * np.abs(w @ x) + (2.0 ** -8 + 2.0 ** -14) * (w @ np.abs(x)))
+
+
+@pytest.mark.parametrize("hkv,d", [(2, 64), (4, 128)])
 @pytest.mark.parametrize("gap", [16.6, 20.6, 23.42, 25.2])
 def test_prompt_many_small_weights_beside_a_large_one(api, hkv, d, gap):
     """A prompt in binary16 whose first token holds nearly all of the weight, the others the rest, which is what the outputs are made
