@@ -40,6 +40,7 @@ constexpr float kShift = 6.f;
 constexpr int kShiftBits = 0x40C00000;
 constexpr float kMaxLead = 8.f;         // how far (base-2 exponent) a score may pass the reference maximum
 constexpr float kSmallestScale = 0x1p-120f;  // a page of V whose scale is below it counts as zeros; so 1 / r is finite
+constexpr float kPart = 0x1p-20f;            // parts of a row are kept times this until they are joined, so that sums of large values stay in range
 constexpr float kMostOutput = 0x1p100f;      // O, in units of r, stays below about this where r falls; what r does not follow is 2^-100 of O
 
 template <int D, int NT>
@@ -529,7 +530,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                         if (g == 0) pm[r] = m[n][k], pl[r] = l[n][k];
 #pragma unroll
                         for (int j = 0; j < VB / 2; ++j)
-                            *reinterpret_cast<float2 *>(po + r * D + VB * g + 2 * j) = make_float2(o[j][n][k] * ref, o[j][n][k + 2] * ref);
+                            *reinterpret_cast<float2 *>(po + r * D + VB * g + 2 * j) = make_float2(o[j][n][k] * kPart * ref, o[j][n][k + 2] * kPart * ref);
                     }
                 }
             if (lane == 0) pieces[warp][slot] = {first_unit, n_tiles, b, head0, rows};
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         }
     };
     auto store_out = [&](const Piece &p, int r, const Sum &x) {
-        const float f = x.l == 0.f ? 0.f : 1.f / x.l;
+        const float f = x.l == 0.f ? 0.f : 1.f / kPart / x.l;
         uint32_t *y = reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + p.b * a.out.token_stride +
                                                    (p.head0 + r) * a.out.head_stride + V * lane);
         if (V == 4) *reinterpret_cast<uint2 *>(y) = make_uint2(E::from_float2(x.o[0] * f, x.o[1] * f), E::from_float2(x.o[V - 2] * f, x.o[V - 1] * f));

@@ -140,6 +140,18 @@ def test_cache_pages_of_a_tile_with_very_different_scales(api, hq, hkv, d, dtype
         check(attend(api, cache, q, d ** -0.5), want, bound)
 
 
+@pytest.mark.parametrize("lens", [[333], [7, 9000], [640] * 40], ids=["333", "7, 9000", "40 x 640"])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 128), (16, 1, 64)])
+@pytest.mark.parametrize("exponent", [121, 100, -90])
+def test_cache_values_at_the_ends_of_bfloat16(api, exponent, hq, hkv, d, lens):
+    """Means of values up to 127 * 2^121, which is near bfloat16's largest, are finite, however the sequence is cut."""
+    cache = Cache(lens, hkv, d, 64, 79)
+    cache.v_scale[:] = 2.0 ** exponent
+    q = torch.randn(len(lens), hq, d, generator=torch.Generator("cuda").manual_seed(83), device="cuda").bfloat16()
+    want, bound = cache.definition(f64(q), 0.05, torch.bfloat16)
+    check(attend(api, cache, q, 0.05), want, bound)
+
+
 def test_appended_values_that_are_tiny(api):
     """What pd_kv_append writes for values near 1e-38 reads as zeros, before, after and without ordinary pages."""
     d, page, n = 64, 32, 96
