@@ -2,8 +2,8 @@
 // tokens j < seq_lens[b], K and V being codes (signed 8 bits) times the scale of their page and head.
 //
 // Bound by memory: every code is read once, 2 * head_dim bytes per token and key/value head, against 4 * group * head_dim
-// operations.  Measured: 64 sequences, 256085 cached tokens, 64 query and 8 key/value heads of 128 (528 MB) 103 us in bursts
-// (5.1 TB/s; 6.8 between segment changes) and 118 at the power limit, where the SM clock falls to 1.74 GHz.
+// operations.  Measured: 64 sequences, 256085 cached tokens, 64 query and 8 key/value heads of 128 (528 MB) 105 us in bursts
+// (6.8 TB/s between segment changes) and 113 sustained, where the power limit takes the SM clock down to 1.74 GHz.
 //
 // Work.  A *segment* is the heads of one sequence that share a key/value head (up to 8 * NT of them); its tokens are cut
 // into tiles of 32.  The tiles of all segments, one after another and with what a segment costs beside them, are dealt to
@@ -91,7 +91,7 @@ __device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return hadd2_u32(prmt
 __device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return hadd2_u32(prmt(w, 0x64646464u, 0x4342), 0xE480E480u); }
 
 // Work is dealt in units: a segment's tiles and, before them, what its beginning and end cost (measured in tiles).
-// In us with 1 / 2 / 4: 64 long sequences with 32 heads on 32 111 / 104 / 106, with 64 on 8 106 / 103 / 102; 96 sequences of
+// In us with 1 / 2 / 4, in short bursts: 64 long sequences with 32 heads on 32 111 / 104 / 106, with 64 on 8 106 / 103 / 102; 96 sequences of
 // 20 to 300 tokens with 64 on 8 23.8 / 23.8 / 25.3.
 constexpr int kSegmentCost = 2;
 // A warp gets so many units at least: with fewer, more parts are to be joined than the shorter ranges save (one token, 64 query

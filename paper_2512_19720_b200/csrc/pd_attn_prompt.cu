@@ -9,10 +9,11 @@
 // end, stays in range beside values of any size.
 //
 // Bound by the tensor cores (4 * head_dim operations per query, key and head) and, as nearly, by the exponentials: a tile of
-// 128 x 128 scores is 1024 clocks of products at head_dim 128 and 1024 clocks of the 16 exponentials a clock that an SM has.
-// Measured: 64 query and 8 key/value heads of 128, one prompt of 8192 tokens 0.93-0.97 ms, 1.1-1.2 PFLOP/s at the power limit
-// (a polynomial for some of the exponentials changed nothing); 7 prompts of 7919 tokens together 222 us; 32 heads, 4 prompts of 512
-// tokens 24 us, where what surrounds the products counts: first loads, the last units of the blocks, instructions not in the cache.
+// 128 x 128 scores is 1024 clocks of products at head_dim 128 and 1024 clocks of the 16 exponentials a clock that an SM has (both
+// pipes are busy 59 % of the time; a polynomial for some of the exponentials changed nothing).
+// Measured, sustained: 64 query and 8 key/value heads of 128, one prompt of 8192 tokens 985 us (1.11 PFLOP/s at the power limit; 850
+// us in short bursts); 7 prompts of 7919 tokens together 257 us (220); 32 heads, 4 prompts of 512 tokens 23.2 us, where what
+// surrounds the products counts: first loads, the last units of the blocks, instructions not in the cache.
 //
 // A block works on units of two *slots* of 128 queries each that read the same keys: two heads that share their key/value
 // head where their number is even, else two consecutive pieces of one head's queries.  Tiles of 128 keys: S = Q K^T (both
@@ -22,7 +23,7 @@
 // Tensor memory: one buffer of 128 columns for S that both slots use in turn (a row of S is taken into registers at once, and
 // the buffer is free again long before its softmax is done), 64 columns of P and 128 of O for each slot.  So the scores of a
 // slot's next tile wait for its softmax, not the softmax for them.  (A buffer of S for each slot with P in its place, where a
-// slot's softmax stands still during its own two products: 1110 us where this gave 900.)
+// slot's softmax stands still during its own two products: 1110 us where this gave 900, 8192 tokens in short bursts.)
 //
 // Roles: warps 0-3 and 4-7 the softmax of slot 0 and 1; warp 8 units and TMA; warps 9 and 10 issue the products with the
 // keys and with the values (one warp for both, scores first: 20 % slower); warp 11 looks for infinities and NaN among the
@@ -119,7 +120,8 @@ __device__ __forceinline__ bool non_finite2(uint32_t w) {
 }
 
 // The products of a group are issued inside one `if (elect_one())` by a warp whose other threads keep to the same path.  Timed
-// with stamps around the issue, products inside `if (lane == 0)` took 105 clocks each, more than the 64 that they run for.
+// with stamps around the issue, products inside `if (lane == 0)` took 105 clocks each, more than the 64 that they run for;
+// with an election for each product the 7 packed prompts take 261 us where one for the group gives 258.
 __device__ __forceinline__ void mma_smem_a(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n"

@@ -12,7 +12,7 @@
 //           sequence) is one round of loads, the page's number comes with the values.
 //   tokens: a warp takes one (sequence, head) of the keys or of the values and walks over its pages, a token at a time
 //           per half warp.  For decode steps: a block per page would mostly wait for four rounds of loads, and half of the
-//           blocks would find nothing to do (64 sequences of one token, 8 heads of 128: 11.4 against 4.5 us).
+//           blocks would find nothing to do.
 // The held codes are read and written again only where the scale grew.
 #include "pd_attn.cuh"
 #include "pd_ptx.cuh"
@@ -25,7 +25,13 @@ namespace {
 constexpr int kVecs = 8;
 constexpr int kMaxThreads = 256;
 constexpr int kTokenWarps = 8;   // tokens: warps of a block
-constexpr int kFewTokens = 4;    // tokens: up to so many new tokens a sequence on average
+// tokens: up to so many new tokens a sequence on average, which is all that the host knows.  Back to back in a graph, heads of
+// 128, pages of 64, us with tokens / with pages:
+//   8 heads, 64 sequences of 1, 4, 8 tokens: 2.2 / 4.7, 3.0 / 4.8, 4.4 / 5.0;  512 of 1, 4: 3.7 / 23.3, 5.2 / 24.3
+//   32 heads, 64 sequences of 1, 4, 8 tokens: 3.1 / 12.4, 4.0 / 12.9, 5.6 / 13.7
+//   8 heads, unequal lengths, where one warp walks over the long piece: 63 of 1 and one of 190: 40 / 5.0;  511 of 1 and one of 1500:
+//   336 / 24.8.  The rule is wrong there; the right one would look at each sequence on the device.
+constexpr int kFewTokens = 4;
 
 // max that hands a NaN on, so that a page with a NaN among its values reads as NaN
 __device__ __forceinline__ float max_nan(float a, float b) {
