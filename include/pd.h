@@ -411,6 +411,8 @@ pd_status pd_attn_prompt_bf16(const void *q, int64_t q_token_stride, int64_t q_h
  * the new ones, whatever the page held before), its held codes become round(c * (s * (1/s'))) and the new ones
  * round(x * (1/s')), all in binary32 with rounding to nearest even.  A page whose s' is below 2^-120 gets codes of zero; one
  * with an infinity or a NaN among its values too, and reads as NaN (an infinite or NaN scale times zero).  No page may belong to two sequences of a call.
+ * A call is made for prompts (a thread block for each page) or for few tokens a sequence (at most 4 on average: a warp for each
+ * sequence and head), whichever its average says: single tokens and long pieces are quicker in two calls than in one.
  */
 pd_status pd_kv_append(const void *k, int64_t k_token_stride, int64_t k_head_stride,
                        const void *v, int64_t v_token_stride, int64_t v_head_stride,

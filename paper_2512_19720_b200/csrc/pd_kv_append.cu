@@ -29,8 +29,9 @@ constexpr int kTokenWarps = 8;   // tokens: warps of a block
 // 128, pages of 64, us with tokens / with pages:
 //   8 heads, 64 sequences of 1, 4, 8 tokens: 2.2 / 4.7, 3.0 / 4.8, 4.4 / 5.0;  512 of 1, 4: 3.7 / 23.3, 5.2 / 24.3
 //   32 heads, 64 sequences of 1, 4, 8 tokens: 3.1 / 12.4, 4.0 / 12.9, 5.6 / 13.7
-//   8 heads, unequal lengths, where one warp walks over the long piece: 63 of 1 and one of 190: 40 / 5.0;  511 of 1 and one of 1500:
-//   336 / 24.8.  The rule is wrong there; the right one would look at each sequence on the device.
+// An average does not show a long piece among single tokens, over which one warp then walks (8 heads, 63 sequences of 1 and one of
+// 190: 40 / 5.0;  511 of 1 and one of 1500: 336 / 24.8): a program that mixes them does better with a call for each kind, until
+// the choice is made for each sequence on the device.
 constexpr int kFewTokens = 4;
 
 // max that hands a NaN on, so that a page with a NaN among its values reads as NaN
