@@ -425,10 +425,11 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                                    for (int k = 0; k < 4; ++k) most = fmaxf(most, fabsf(o[j][n][k] * factor[n][k & 1]));
+                                    for (int k = 0; k < 4; ++k)
+                                        if (n * 8 + 2 * t + (k & 1) < rows) most = fmaxf(most, fabsf(o[j][n][k] * factor[n][k & 1]));
 #pragma unroll
                             for (int d = 1; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-                            step = most > 0.f ? fmaxf(fminf(step, kMostOutput / most), 1.f) : 1.f;
+                            step = most > 0.f ? fmaxf(fminf(fminf(step, kMostOutput / most), 0x1p120f), 1.f) : 1.f;  // finite, however little is left of O
                             ref = most > 0.f ? fmaxf(sv_hi, ref / step) : sv_hi;
                             if (most == 0.f) ref_top = 0.f;
                         } else {

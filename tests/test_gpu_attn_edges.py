@@ -152,6 +152,29 @@ def test_cache_values_at_the_ends_of_bfloat16(api, exponent, hq, hkv, d, lens):
     check(attend(api, cache, q, 0.05), want, bound)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (12, 1, 64), (16, 2, 128)])
+@pytest.mark.parametrize("first,then", [(2.0 ** 100, 2.0 ** -119), (2.0 ** 60, 2.0 ** -119), (1.0, 2.0 ** -119), (2.0 ** -119, 2.0 ** 100)])
+@pytest.mark.parametrize("leads", [(30.0, 10.0, -30.0, 0.0), (30.0, 25.0, 28.0, 30.0), (150.0, 140.0, 150.0, 150.0)], ids=["some", "all", "far"])
+def test_cache_weights_that_vanish_beside_scales_that_fall(api, leads, first, then, hq, hkv, d):
+    """Some heads, or all of them, leave the first pages behind by up to e^300 when the scales of V change: every sequence is whole in a warp."""
+    n_seqs, page = 1600, 32
+    cache = Cache([4 * page] * n_seqs, hkv, d, page, 89)
+    early = np.arange(4 * n_seqs) % 4 < 2
+    cache.v_scale[early], cache.v_scale[~early], cache.k_scale[:] = np.float32(first), np.float32(then), 2.0 ** -6
+    cache.k_codes[early, ..., 0], cache.k_codes[~early, ..., 0] = -64, 64
+    q = 0.1 * torch.randn(n_seqs, hq, d, generator=torch.Generator("cuda").manual_seed(97), device="cuda")
+    q[..., 0] = torch.tensor(leads, device="cuda").repeat(hq // 4)
+    q = q.bfloat16()
+    got = attend(api, cache, q, 1.0)
+    assert bool(torch.isfinite(got).all())
+    some = [0, 1, 77, n_seqs - 1]
+    part = Cache([4 * page] * len(some), hkv, d, page, 0)
+    for name in ("k_codes", "v_codes", "k_scale", "v_scale"):
+        setattr(part, name, getattr(cache, name)[cache.table[some].reshape(-1)])
+    want, bound = part.definition(f64(q[some]), 1.0, torch.bfloat16)
+    check(got[some], want, bound)
+
+
 def test_appended_values_that_are_tiny(api):
     """What pd_kv_append writes for values near 1e-38 reads as zeros, before, after and without ordinary pages."""
     d, page, n = 64, 32, 96
