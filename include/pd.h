@@ -67,7 +67,8 @@ typedef enum {
     PD_OP_MERGE = 3,
     PD_OP_FIT = 4,       /* pd_fit_loss_grad: M = tokens of the batch */
     PD_OP_FIT_LAYER = 5, /* pd_fit_layer: M = max(batch, M_val) */
-    PD_OP_ATTN = 6       /* pd_attn_prompt, pd_kv_append, pd_attn_cache: any sizes */
+    PD_OP_ATTN = 6,      /* pd_attn_prompt, pd_kv_append, pd_attn_cache, pd_rope, pd_kv_append_rope: any sizes */
+    PD_OP_ATTN_CHUNK = 7 /* pd_attn_chunk: any sizes */
 } pd_op;
 
 /*
@@ -449,6 +450,95 @@ pd_status pd_attn_cache_bf16(const void *q, int64_t q_token_stride, int64_t q_he
                              const int32_t *block_table, int64_t table_stride, int32_t table_width, void *out,
                              int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes,
                              void *cuda_stream);
+
+/*
+ * ---- Positions, and pieces of sequences ----
+ * A sequence's tokens may come in pieces: a long prompt read a piece at a time, a conversation's next turn, a few drafted tokens that
+ * are checked together, single tokens, all in one batch.  pd_kv_append_rope (or pd_rope and pd_kv_append) puts a piece's keys and values
+ * into the cache, pd_attn_chunk attends with its queries over the cache.  Sizes, cache and packing are those above.
+ *
+ * Rotation.  Of a head's head_dim values the first 2 * pairs turn, the others stay as they are.  Pair i is (i, i + pairs), or
+ * (2 i, 2 i + 1) with interleaved = 1; (x, y) becomes (x cos t - y sin t, x sin t + y cos t) with t = positions[axes[i]][token] * inv_freq[i].
+ *   positions : int32, n_axes rows of one number for each token, axis_stride apart (not looked at with one axis); any values
+ *   axes      : int32 [pairs], which row a pair turns with (time, height and width of a picture's patches); may be NULL with one axis
+ *   inv_freq  : fp32 [pairs]
+ *   pairs     : a multiple of 8, at most head_dim / 2
+ * Angles are computed in binary64 and brought to half a turn there, sines, cosines and the rotation in binary32.  An entry of
+ * axes outside [0, n_axes) latches PD_ERR_BAD_INDEX and counts as 0.
+ */
+
+/*
+ * pd_rope -- turns queries and keys.
+ *
+ *   q : in, [n_tokens, q_heads, head_dim];  k : in, [n_tokens, k_heads, head_dim], not looked at where k_heads is 0
+ *   q_out, k_out : out, the same shapes; each may be its input itself (the same pointer and strides), and must not overlap it otherwise
+ *   inverse : 1 turns back, which is also the gradient with respect to q and k of a loss whose gradient with respect to the outputs is given
+ * Workspace: PD_OP_ATTN.
+ */
+pd_status pd_rope(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                  const int32_t *positions, int64_t axis_stride, int32_t n_axes, const int32_t *axes, const float *inv_freq, int32_t pairs,
+                  int32_t interleaved, int32_t inverse, int64_t n_tokens, int32_t q_heads, int32_t k_heads, int32_t head_dim,
+                  void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                  void *k_out, int64_t k_out_token_stride, int64_t k_out_head_stride,
+                  void *workspace, size_t workspace_bytes, void *cuda_stream);
+pd_status pd_rope_bf16(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                       const int32_t *positions, int64_t axis_stride, int32_t n_axes, const int32_t *axes, const float *inv_freq, int32_t pairs,
+                       int32_t interleaved, int32_t inverse, int64_t n_tokens, int32_t q_heads, int32_t k_heads, int32_t head_dim,
+                       void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                       void *k_out, int64_t k_out_token_stride, int64_t k_out_head_stride,
+                       void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * pd_kv_append_rope -- turns queries and keys and quantises the turned keys and the values into the cache, in one launch.
+ *
+ *   q, q_out : queries, turned into q_out (which may be q itself) in the rows that a sequence claims; not looked at where q_heads is 0
+ *   positions : NULL: a token turns with its place in its sequence, seq_lens[b] - (cu_seqlens[b + 1] - cu_seqlens[b]) for the first new one
+ * Everything else as in pd_kv_append, with the turned keys in binary32 (they are not rounded to 16 bits before they are quantised) in the place
+ * of k; k_values are the turned keys that the codes stand for.  Sequences with few new tokens and long pieces may be mixed freely.
+ * Workspace: PD_OP_ATTN.
+ */
+pd_status pd_kv_append_rope(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                            const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                            const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                            const int32_t *positions, int64_t axis_stride, int32_t n_axes, const int32_t *axes, const float *inv_freq, int32_t pairs,
+                            int32_t interleaved, int8_t *k_codes, int8_t *v_codes, float *k_scale, float *v_scale, int64_t n_pages, int32_t page,
+                            const int32_t *seq_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                            void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                            void *k_values, void *v_values, void *workspace, size_t workspace_bytes, void *cuda_stream);
+pd_status pd_kv_append_rope_bf16(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                                 const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                                 const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                 const int32_t *positions, int64_t axis_stride, int32_t n_axes, const int32_t *axes, const float *inv_freq, int32_t pairs,
+                                 int32_t interleaved, int8_t *k_codes, int8_t *v_codes, float *k_scale, float *v_scale, int64_t n_pages, int32_t page,
+                                 const int32_t *seq_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                                 void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                                 void *k_values, void *v_values, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * pd_attn_chunk -- attention of several new tokens per sequence over the cache that holds them already.
+ *
+ *   q   : in,  [n_tokens, q_heads, head_dim], packed by cu_seqlens: the last cu_seqlens[b + 1] - cu_seqlens[b] tokens of sequence b,
+ *         which has seq_lens[b] in all; none, one or many
+ *   max_new : the most new tokens of a sequence, 0 for not known
+ *   out : out, [n_tokens, q_heads, head_dim]: token i of the n new ones attends to the cached tokens 0 .. seq_lens[b] - n + i
+ * Rows of n_tokens that no sequence claims are left as they are.  Slots of a page behind what a token attends to and pages that it does not
+ * reach have no influence on it, whatever they hold; a page whose scale is not finite makes the tokens that attend to any of it NaN.
+ * Weights are rounded to binary16 (relative to the largest, times the scale of V's page, times 2^7) for their product with V; pages whose scale of V is below 2^-67 of the
+ * largest of the sequence lose precision.  Offsets that decrease, more new tokens than max_new or than seq_lens[b] and lengths beyond the table
+ * latch PD_ERR_BAD_INDEX, and the sequence is left out.  The same call gives the same bits.
+ * Workspace: pd_workspace_bytes(PD_OP_ATTN_CHUNK, 0, 0, 0, 0) bytes (about 40 MB, for parts of rows whose keys are dealt to several blocks), of
+ * which only the status words have to be zero before the first call.
+ */
+pd_status pd_attn_chunk(const void *q, int64_t q_token_stride, int64_t q_head_stride, const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens,
+                        int64_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale, const int8_t *k_codes,
+                        const int8_t *v_codes, const float *k_scale, const float *v_scale, int64_t n_pages, int32_t page,
+                        const int32_t *seq_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width, void *out,
+                        int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *cuda_stream);
+pd_status pd_attn_chunk_bf16(const void *q, int64_t q_token_stride, int64_t q_head_stride, const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens,
+                             int64_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale, const int8_t *k_codes,
+                             const int8_t *v_codes, const float *k_scale, const float *v_scale, int64_t n_pages, int32_t page,
+                             const int32_t *seq_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width, void *out,
+                             int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* Human-readable name of a status code; never NULL. */
 const char *pd_status_string(pd_status status);

@@ -61,3 +61,28 @@ def attn_cache(q, k_codes, v_codes, k_scale, v_scale, lens, table, scale):
             v = np.concatenate([v_codes[p, h // group].astype(np.float64) * float(v_scale[p, h // group]) for p in pages])[:n]
             out[b, h] = softmax_weights(k @ q[b, h] * scale) @ v
     return out
+
+
+def rope(x, positions, inv_freq, axes, interleaved, inverse=False):
+    """x [T, heads, d] (fp64), positions [n_axes, T], inv_freq [pairs], axes [pairs]: each pair of each token by itself."""
+    out = x.copy()
+    pairs = len(inv_freq)
+    for t in range(x.shape[0]):
+        for i in range(pairs):
+            a = float(positions[axes[i]][t]) * float(inv_freq[i]) * (-1 if inverse else 1)
+            p, q = (2 * i, 2 * i + 1) if interleaved else (i, i + pairs)
+            out[t, :, p] = x[t, :, p] * np.cos(a) - x[t, :, q] * np.sin(a)
+            out[t, :, q] = x[t, :, p] * np.sin(a) + x[t, :, q] * np.cos(a)
+    return out
+
+
+def attn_chunk(q, k_codes, v_codes, k_scale, v_scale, lens, new, table, scale):
+    """q [T, Hq, d] (fp64): the last new[b] of the lens[b] tokens of each sequence, which are all in the cache."""
+    out = np.zeros_like(q)
+    at = 0
+    for b, (n, m) in enumerate(zip(lens, new)):
+        for i in range(m):
+            one = attn_cache(q[at + i:at + i + 1], k_codes, v_codes, k_scale, v_scale, [n - m + i + 1], table[b:b + 1], scale)
+            out[at + i] = one[0]
+        at += m
+    return out

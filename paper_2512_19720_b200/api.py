@@ -14,7 +14,7 @@ import torch
 AXIS_ROW = 0
 AXIS_COL = 1
 AXIS_SCALAR = 2  # pd_fit_* only
-OP_PACK, OP_LINEAR, OP_LINEAR_MULTIVARIANT, OP_MERGE, OP_FIT, OP_FIT_LAYER, OP_ATTN = 0, 1, 2, 3, 4, 5, 6
+OP_PACK, OP_LINEAR, OP_LINEAR_MULTIVARIANT, OP_MERGE, OP_FIT, OP_FIT_LAYER, OP_ATTN, OP_ATTN_CHUNK = 0, 1, 2, 3, 4, 5, 6, 7
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpd.so")
@@ -24,7 +24,8 @@ EXPORTS = ["pd_pack_delta", "pd_pack_delta_static", "pd_linear_host", "pd_linear
            "pd_pack_delta_bf16", "pd_merge_bf16", "pd_linear_bf16", "pd_linear_multivariant_bf16",
            "pd_artifact_bytes", "pd_load_merged",
            "pd_transpose_mask", "pd_fit_loss_grad", "pd_fit_adamw_step", "pd_fit_layer",
-           "pd_attn_prompt", "pd_attn_prompt_bf16", "pd_kv_append", "pd_kv_append_bf16", "pd_attn_cache", "pd_attn_cache_bf16"]
+           "pd_attn_prompt", "pd_attn_prompt_bf16", "pd_kv_append", "pd_kv_append_bf16", "pd_attn_cache", "pd_attn_cache_bf16",
+           "pd_rope", "pd_rope_bf16", "pd_kv_append_rope", "pd_kv_append_rope_bf16", "pd_attn_chunk", "pd_attn_chunk_bf16"]
 LINEAR_WEIGHTS_RESIDENT = 1
 
 
@@ -86,11 +87,14 @@ def _load() -> ctypes.CDLL:
     lib.pd_fit_adamw_step.restype = ctypes.c_int
     lib.pd_fit_layer.argtypes = [p, p, i64, p, p, i64, p, p, p, p, i64, i64, i32, i64, ctypes.POINTER(PdAdamW), i32, p, p, p, p, sz, p]
     lib.pd_fit_layer.restype = ctypes.c_int
-    f32, view = ctypes.c_float, [p, i64, i64]
+    f32, view, turns, cache = ctypes.c_float, [p, i64, i64], [p, i64, i32, p, p, i32, i32], 4 * [p] + [i64, i32, p, p, i64, i32]
     for suffix in ("", "_bf16"):
         for name, argtypes in (("pd_attn_prompt", 3 * view + [p, i32, i64, i32, i32, i32, f32] + view + [p, sz, p]),
                                ("pd_kv_append", 2 * view + [p, i32, i64, i32, i32] + 4 * [p] + [i64, i32, p, p, i64, i32] + 2 * [p] + [p, sz, p]),
-                               ("pd_attn_cache", view + [i32, i32, i32, i32, f32] + 4 * [p] + [i64, i32, p, p, i64, i32] + view + [p, sz, p])):
+                               ("pd_attn_cache", view + [i32, i32, i32, i32, f32] + 4 * [p] + [i64, i32, p, p, i64, i32] + view + [p, sz, p]),
+                               ("pd_rope", 2 * view + turns + [i32, i64, i32, i32, i32] + 2 * view + [p, sz, p]),
+                               ("pd_kv_append_rope", 3 * view + [p, i32, i64, i32, i32, i32] + turns + cache + view + 2 * [p] + [p, sz, p]),
+                               ("pd_attn_chunk", view + [p, i32, i64, i64, i32, i32, i32, f32] + cache + view + [p, sz, p])):
             fn = getattr(lib, name + suffix)
             fn.argtypes, fn.restype = argtypes, ctypes.c_int
     lib.pd_launch_count.argtypes = []
@@ -372,15 +376,23 @@ _HALF_TYPES = (torch.float16, torch.bfloat16)
 _get_device, _raw_stream, _capturing = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch._C._cuda_isCurrentStreamCapturing
 
 
-def _attn_workspace(index: int, stream: int):
+_chunk_ws_cache: dict = {}
+_chunk_graph_ws: dict = {}
+
+
+def _attn_workspace(index: int, stream: int, op: int = OP_ATTN):
     """The attention calls' own scratch tensor with its address and size, one for each device and stream: it must be all
     zero before its first call, and calls that overlap on the GPU must not share it.  Calls that are captured get one of
     their graph's own, since graphs are replayed in any order and on any stream: each replay zeroes it first."""
     capture = lib.pd_capture_id(stream) if stream else 0  # the default stream cannot be captured
-    cache = _attn_graph_ws if capture else _attn_ws_cache
+    cache = (_chunk_graph_ws if capture else _chunk_ws_cache) if op == OP_ATTN_CHUNK else (_attn_graph_ws if capture else _attn_ws_cache)
     ws = cache.get((index, stream))
     if ws is None or ws[3] != capture:
-        t = torch.zeros(workspace_bytes(OP_ATTN), dtype=torch.uint8, device=torch.device("cuda", index))
+        if op == OP_ATTN_CHUNK:  # of which only the status words have to be zero
+            t = torch.empty(workspace_bytes(op), dtype=torch.uint8, device=torch.device("cuda", index))
+            t[:256].zero_()
+        else:
+            t = torch.zeros(workspace_bytes(op), dtype=torch.uint8, device=torch.device("cuda", index))
         ws = cache[index, stream] = (t, t.data_ptr(), t.numel(), capture)
     return ws
 
@@ -390,6 +402,12 @@ def attn_workspace(device=None) -> torch.Tensor:
     captured graph's own is zeroed at every replay, its status too: give a workspace to calls whose status is to be read."""
     index = torch.cuda.current_device() if device is None or device.index is None else device.index
     return _attn_workspace(index, _raw_stream(index))[0]
+
+
+def chunk_workspace(device=None) -> torch.Tensor:
+    """attn_workspace's counterpart for pd_attn_chunk."""
+    index = torch.cuda.current_device() if device is None or device.index is None else device.index
+    return _attn_workspace(index, _raw_stream(index), OP_ATTN_CHUNK)[0]
 
 
 def _heads(t, name, dtype, index):
@@ -441,15 +459,15 @@ def _cache(k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index, seq_le
             block_table.data_ptr(), table_strides[0] if n_seqs > 1 else width, width)
 
 
-def _attn_call(name, fn, index, args, workspace):
+def _attn_call(name, fn, index, args, workspace, op=OP_ATTN):
     """Calls an entry point with `args`, a workspace and the current stream of device `index`."""
     if _get_device() != index:
         with torch.cuda.device(index):
-            return _attn_call(name, fn, index, args, workspace)
+            return _attn_call(name, fn, index, args, workspace, op)
     stream = _raw_stream(index)
     if workspace is None:
-        ws = None if stream and _capturing() else _attn_ws_cache.get((index, stream))
-        _, ptr, size, _ = ws or _attn_workspace(index, stream)
+        ws = None if stream and _capturing() else (_attn_ws_cache if op == OP_ATTN else _chunk_ws_cache).get((index, stream))
+        _, ptr, size, _ = ws or _attn_workspace(index, stream, op)
     else:
         ptr, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     code = fn(*args, ptr, size, stream)
@@ -508,6 +526,98 @@ def pd_attn_cache(q, k_codes, v_codes, k_scale, v_scale, seq_lens, block_table, 
     codes = _cache(k_codes, v_codes, k_scale, v_scale, None, head_dim, index, seq_lens, block_table, n_seqs)
     args = view + (n_seqs, q_heads, k_codes.shape[1], head_dim, head_dim ** -0.5 if scale is None else scale) + codes + _heads(out, "out", dtype, index)
     _attn_call("pd_attn_cache", lib.pd_attn_cache_bf16 if dtype is torch.bfloat16 else lib.pd_attn_cache, index, args, workspace)
+    return out
+
+
+def _rotation(positions, inv_freq, axes, interleaved, index, n_tokens):
+    """What the entry points take of a rotation."""
+    pairs = inv_freq.numel()
+    freq = _flat(inv_freq, "inv_freq", torch.float32, index, (pairs,))
+    axes_ptr = None if axes is None else _flat(axes, "axes", torch.int32, index, (pairs,))
+    if positions is None:
+        return None, 0, 1, axes_ptr, freq, pairs, 1 if interleaved else 0
+    shape, strides = positions.shape, positions.stride()
+    if positions.dtype is not torch.int32 or positions.get_device() != index:
+        raise TypeError(f"positions must be an int32 tensor on CUDA device {index}: got {positions.dtype} on {positions.device}")
+    if len(shape) not in (1, 2) or shape[-1] != n_tokens or (n_tokens > 1 and strides[-1] != 1) or shape[0] == 0 and len(shape) == 2:
+        raise ValueError(f"positions: [{n_tokens}] or [axes, {n_tokens}] with contiguous rows is wanted: got shape {tuple(shape)}, strides {strides}")
+    if len(shape) == 1:
+        return positions.data_ptr(), n_tokens, 1, axes_ptr, freq, pairs, 1 if interleaved else 0
+    return positions.data_ptr(), strides[0] if shape[0] > 1 else n_tokens, shape[0], axes_ptr, freq, pairs, 1 if interleaved else 0
+
+
+def _out_like(out, x, name):
+    if out is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    if out.shape != x.shape:
+        raise ValueError(f"{name}: shape {tuple(out.shape)}, wanted {tuple(x.shape)}")
+    return out
+
+
+def pd_rope(q, k, positions, inv_freq, axes=None, interleaved=False, inverse=False, q_out=None, k_out=None, workspace=None):
+    """Turns q [T, q_heads, head_dim] and k [T, k_heads, head_dim] (or None): pair i of a head by positions[axes[i]] * inv_freq[i].
+    positions int32 [T] or [n_axes, T], inv_freq fp32 [pairs], axes int32 [pairs].  q_out and k_out may be q and k.  inverse turns back:
+    the gradient's way.  Returns (q_out, k_out)."""
+    dtype, index, shape = q.dtype, q.get_device(), q.shape
+    view = _heads(q, "q", dtype, index)
+    n_tokens, q_heads, head_dim = shape
+    if positions is None:
+        raise ValueError("positions: a tensor is wanted")
+    q_out = _out_like(q_out, q, "q_out")
+    if k is None:
+        k_view, k_out_view, k_heads, k_out = (None, 0, 0), (None, 0, 0), 0, None
+    else:
+        k_view, k_heads = _heads(k, "k", dtype, index), k.shape[1]
+        if k.shape[0] != n_tokens or k.shape[2] != head_dim:
+            raise ValueError(f"shapes do not fit: q {tuple(shape)}, k {tuple(k.shape)}")
+        k_out = _out_like(k_out, k, "k_out")
+        k_out_view = _heads(k_out, "k_out", dtype, index)
+    args = view + k_view + _rotation(positions, inv_freq, axes, interleaved, index, n_tokens) + (
+        1 if inverse else 0, n_tokens, q_heads, k_heads, head_dim) + _heads(q_out, "q_out", dtype, index) + k_out_view
+    _attn_call("pd_rope", lib.pd_rope_bf16 if dtype is torch.bfloat16 else lib.pd_rope, index, args, workspace)
+    return q_out, k_out
+
+
+def pd_kv_append_rope(q, k, v, k_codes, v_codes, k_scale, v_scale, cu_seqlens, seq_lens, block_table, inv_freq, positions=None, axes=None, interleaved=False,
+                      q_out=None, k_values=None, v_values=None, workspace=None):
+    """pd_kv_append of turned keys, with the queries q [T, q_heads, head_dim] (or None) turned on the way into q_out (which may be q).
+    Rotation as in pd_rope; without positions a token turns with its place in its sequence.  k_values: the turned keys that the new codes
+    stand for.  Returns q_out."""
+    dtype, index, shape = k.dtype, k.get_device(), k.shape
+    views = _heads(k, "k", dtype, index) + _heads(v, "v", dtype, index)
+    if shape != v.shape:
+        raise ValueError(f"shapes do not fit: k {tuple(shape)}, v {tuple(v.shape)}")
+    n_tokens, kv_heads, head_dim = shape
+    n_seqs = seq_lens.numel()
+    if q is None:
+        q_view, out_view, q_heads, q_out = (None, 0, 0), (None, 0, 0), 0, None
+    else:
+        q_view, q_heads = _heads(q, "q", dtype, index), q.shape[1]
+        if q.shape[0] != n_tokens or q.shape[2] != head_dim:
+            raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(shape)}")
+        q_out = _out_like(q_out, q, "q_out")
+        out_view = _heads(q_out, "q_out", dtype, index)
+    args = q_view + views + (_flat(cu_seqlens, "cu_seqlens", torch.int32, index, (n_seqs + 1,)), n_seqs, n_tokens, q_heads, kv_heads, head_dim) + _rotation(
+        positions, inv_freq, axes, interleaved, index, n_tokens) + _cache(
+        k_codes, v_codes, k_scale, v_scale, kv_heads, head_dim, index, seq_lens, block_table, n_seqs) + out_view + (
+        None if k_values is None else _flat(k_values, "k_values", dtype, index, shape), None if v_values is None else _flat(v_values, "v_values", dtype, index, shape))
+    _attn_call("pd_kv_append_rope", lib.pd_kv_append_rope_bf16 if dtype is torch.bfloat16 else lib.pd_kv_append_rope, index, args, workspace)
+    return q_out
+
+
+def pd_attn_chunk(q, k_codes, v_codes, k_scale, v_scale, cu_seqlens, seq_lens, block_table, max_new=0, scale=None, out=None, workspace=None):
+    """Attention of the new tokens q [T, q_heads, head_dim] (packed by cu_seqlens; the last ones of each sequence of seq_lens[b] tokens) over the
+    cache, which holds them already: each attends to itself and what is before it.  max_new: the most new tokens of a sequence, 0 for not
+    known.  Returns out [T, q_heads, head_dim]."""
+    dtype, index, shape = q.dtype, q.get_device(), q.shape
+    view = _heads(q, "q", dtype, index)
+    n_tokens, q_heads, head_dim = shape
+    n_seqs = seq_lens.numel()
+    out = _out_like(out, q, "out")
+    codes = _cache(k_codes, v_codes, k_scale, v_scale, None, head_dim, index, seq_lens, block_table, n_seqs)
+    args = view + (_flat(cu_seqlens, "cu_seqlens", torch.int32, index, (n_seqs + 1,)), n_seqs, n_tokens, max_new, q_heads, k_codes.shape[1], head_dim,
+                   head_dim ** -0.5 if scale is None else scale) + codes + _heads(out, "out", dtype, index)
+    _attn_call("pd_attn_chunk", lib.pd_attn_chunk_bf16 if dtype is torch.bfloat16 else lib.pd_attn_chunk, index, args, workspace, OP_ATTN_CHUNK)
     return out
 
 

@@ -14,8 +14,7 @@
 //           per half warp.  For decode steps: a block per page would mostly wait for four rounds of loads, and half of the
 //           blocks would find nothing to do.
 // The held codes are read and written again only where the scale grew.
-#include "pd_attn.cuh"
-#include "pd_ptx.cuh"
+#include "pd_kv_quant.cuh"
 
 namespace pd {
 namespace {
@@ -34,20 +33,6 @@ constexpr int kTokenWarps = 8;   // tokens: warps of a block
 // the choice is made for each sequence on the device.
 constexpr int kFewTokens = 4;
 
-// max that hands a NaN on, so that a page with a NaN among its values reads as NaN
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-
-// Rounding to a whole number (to nearest even) by adding 1.5 * 2^23: the sum's low byte is the code.  A conversion
-// instruction runs at an eighth of the rate.
-constexpr float kShift = 12582912.f;
-__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
-    return prmt(prmt(__float_as_uint(a), __float_as_uint(b), 0x0040), prmt(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
-}
-
 // The largest magnitude, two at a time: without their signs the 16-bit values order like whole numbers, a NaN above all.
 __device__ __forceinline__ uint32_t magnitude2(const uint4 &raw, uint32_t most) {
     return __vmaxu2(__vmaxu2(__vmaxu2(raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu), __vmaxu2(raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu)), most);
@@ -57,15 +42,6 @@ __device__ __forceinline__ float warp_magnitude(uint32_t most) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, d));
     return Elem<BF16>::to_float(static_cast<unsigned short>(max(most & 0xffffu, most >> 16)));
-}
-
-struct Scale {
-    float s, inv;    // 1 / s; 0 where s is too small for it, infinite or NaN
-    uint32_t keep;   // bits of the codes: none where inv is 0, so that an infinite scale times any code of the page is NaN too
-};
-__device__ __forceinline__ Scale scale_of(float s_old, float amax) {
-    const float s = max_nan(s_old, __fdiv_rn(amax, 127.f)), inv = s >= 0x1p-120f ? __frcp_rn(s) : 0.f;
-    return {s, inv, inv > 0.f ? 0xffffffffu : 0u};
 }
 
 // eight values to their codes and, unless nullptr, to the values that those stand for
@@ -86,26 +62,6 @@ __device__ __forceinline__ void store8(const uint4 &raw, const Scale &sc, int8_t
         for (int j = 0; j < 4; ++j) o[j] = E::from_float2((f[2 * j] - kShift) * sc.s, (f[2 * j + 1] - kShift) * sc.s);
         *reinterpret_cast<uint4 *>(values) = make_uint4(o[0], o[1], o[2], o[3]);
     }
-}
-
-// sixteen held codes of the smaller scale s_old to those of the larger one
-__device__ __forceinline__ void scale_again16(uint4 *p, float s_old, const Scale &sc) {
-    const float ratio = s_old * sc.inv;
-    const uint4 c = *p;
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    uint32_t r[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        float f[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[k] = __fadd_rn(__fmul_rn(static_cast<float>(static_cast<int8_t>(w[j] >> (8 * k))), ratio), kShift);
-        r[j] = low_bytes(f[0], f[1], f[2], f[3]) & sc.keep;
-    }
-    *p = make_uint4(r[0], r[1], r[2], r[3]);
-}
-
-__device__ __forceinline__ bool bad_lengths(const AppendArgs &a, int first, int last, int len) {
-    return first < 0 || last < first || last > a.n_tokens || len < last - first;
 }
 
 template <int D, bool BF16>
