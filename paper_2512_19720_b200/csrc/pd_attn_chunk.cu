@@ -17,9 +17,8 @@
 // The keys of all units, one unit after another, are dealt to the blocks in ranges of equal cost whatever the lengths are; where a
 // range ends inside a unit the parts are joined by a second kernel, in the order of the keys: results do not depend on the schedule.
 //
-// Roles: warps 0-3 and 4-7 the softmax of slot 0 and 1, and the outputs; warp 8 units, pages and copies; warps 9 and 10 the products with the keys
-// and with the values; warps 12-15 turn codes into 16-bit operands.  Codes come by bulk copies, page by page, into a ring; converted
-// tiles of 128 tokens, keys and values in turn, into another.  Every wait is bounded.
+// Roles: warps 0-3 and 4-7 the softmax of slot 0 and 1, and the outputs; warp 8 units and pages; warp 11 copies; warps 9 and 10 the products with the keys
+// and with the values; warps 12-15 turn codes into 16-bit operands.  Every wait on another role is bounded.
 #include "pd_attn.cuh"
 #include "pd_attn_mma.cuh"
 
@@ -29,8 +28,8 @@ namespace {
 constexpr int kTile = 128;  // rows of a slot, keys of a tile
 constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
-constexpr int kSteps = 6;      // steps that the producer may be ahead
-constexpr int kReaders = 14;   // warps that read a step
+constexpr int kSteps = 6;       // steps that the producer may be ahead
+constexpr int kReaders = 15;   // warps that read a step
 constexpr int kMaxGrid = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLead = 8.f;  // how far (base-2 exponent) a score may pass the reference maximum
@@ -57,19 +56,22 @@ struct Step {
     int head, n_heads;     // first query head and heads of the rows
     int part;              // where a part of a unit goes; -1: the whole unit, written to out
     int tainted;           // first key of a page whose scale is not finite
-    int zero;              // bit g: the values of keys 16 g .. of the tile are zero
-    int pad[5];
-    float4 group[8];       // keys 16 g .. 16 g + 15: factor of the scores, log2(s_v / r), r / s_v
+    int pad[2];
+    // for keys 16 g .. 16 g + 15 of the tile
+    float4 factor[8];      // of the scores, twice, and log2(s_v / r), twice: pairs as the packed arithmetic takes them
+    float weight[8];       // r / s_v
+    uint32_t place[8];     // of their codes, in blocks of 16 keys from the cache's first; kNoKeys; kZeroValues: the values are zero whatever their codes are
 };
-static_assert(sizeof(Step) == 192, "layout");
+static_assert(sizeof(Step) == 240, "layout");
+constexpr uint32_t kNoKeys = 0xffffffffu, kZeroValues = 0x80000000u;
 
 struct Bars {
     uint64_t step_full[kSteps], step_empty[kSteps];
-    uint64_t raw_full[8], raw_empty[8], kv_full[8], kv_empty[8];
+    uint64_t raw_full[8], raw_empty[8];
+    uint64_t kv_full[8], kv_empty[8];
     uint64_t q_full, q_empty, s_full[2], s_free, p_half[2][2], o_done[2], o_last, o_empty[2], joined;
     uint32_t tmem;
     int abort_flag;
-    int64_t warp_sum[kWarps];
 };
 
 template <int D>
@@ -82,14 +84,29 @@ struct ChunkSmem {
     static constexpr int kStepRing = kRawRing + kRaw * kRawBytes;
     static constexpr int kSums = kStepRing + kSteps * static_cast<int>(sizeof(Step));  // m and l of slot 1's rows, by keys
     static constexpr int kBars = kSums + kTile * 8 + 16;
-    static constexpr int kTotal = kBars + 640;
+    static constexpr int kTotal = kBars + 512;
     static constexpr int kScan = kRawRing;  // costs before each thread's share of the sequences, until the first unit is found
-    static_assert(sizeof(Bars) <= 640 && kTotal <= 227 * 1024 && kThreads * 8 <= kRaw * kRawBytes, "shared memory");
+    static_assert(sizeof(Bars) <= 512 && kTotal <= 227 * 1024 && (kThreads + kWarps) * 8 <= kRaw * kRawBytes, "shared memory");
 };
 
 // A part of a unit: rows of O (binary32, in units of r) as [head_dim / 4][256 rows][4], then {m, l, ref, -} of each row.
 template <int D>
 constexpr int kPartFloats = 256 * D + 256 * 4;
+
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+    uint2 x;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(at) : "memory");
+    return x;
+}
+__device__ __forceinline__ void sts128(uint32_t at, const uint4 &x) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+
+__device__ __forceinline__ uint32_t clock32() {
+    uint32_t t;
+    asm volatile("mov.u32 %0, %%clock;" : "=r"(t));
+    return t;
+}
 
 // Units of a sequence's rows that read one key/value head (a *stream*), and what they cost.
 struct Stream {
@@ -129,16 +146,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
     const int per_seq = a.kv_heads * chunks;  // streams
     const int page = 1 << a.page_log2;
     const int64_t room = static_cast<int64_t>(a.table_width) << a.page_log2;
-    // Bounded; the first one to give up says where, and the block's last act is to report it.
+    // Bounded; the first one to give up says where, and the block's last act is to report it.  Short, because it is in the code of every
+    // role many times over.
     auto wait = [&](uint64_t *b, uint32_t parity, int where) {
-        if (mbar_try_wait(b, parity & 1u)) return true;
-        const long long since = clock64();
-        while (!mbar_try_wait(b, parity & 1u))
-            if (clock64() - since > kWaitCycles) {
-                *abort_flag = where;
-                return false;
-            }
-        return true;
+        const uint32_t since = clock32();
+        bool done;
+        while (!(done = mbar_try_wait(b, parity & 1u)) && clock32() - since <= static_cast<uint32_t>(kWaitCycles)) {}
+        if (!done) *abort_flag = where;
+        return done;
     };
     auto wait_warp = [&](uint64_t *b, uint32_t parity, int where) { return __all_sync(0xffffffffu, wait(b, parity, where)) != 0; };
 
@@ -169,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         else if (blockIdx.x == 0) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
         return s;
     };
-    int64_t *scan = reinterpret_cast<int64_t *>(smem + L::kScan);
+    int64_t *scan = reinterpret_cast<int64_t *>(smem + L::kScan), *warp_sum = scan + kThreads;
     const int share = (a.n_seqs + kThreads - 1) / kThreads;
     int64_t sum = 0;
     for (int b = threadIdx.x * share; b < min(a.n_seqs, static_cast<int>(threadIdx.x + 1) * share); ++b) {
@@ -182,14 +197,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         const int64_t up = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += up;
     }
-    if (lane == 31) bar.warp_sum[warp] = incl;
+    if (lane == 31) warp_sum[warp] = incl;
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
     int64_t before = 0, total = 0;
     for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) before += bar.warp_sum[w];
-        total += bar.warp_sum[w];
+        if (w < warp) before += warp_sum[w];
+        total += warp_sum[w];
     }
     scan[threadIdx.x] = before + incl - sum;
     __syncthreads();
@@ -208,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
     };
 
     if (warp >= 8 && warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 8) {
         // ------------------------------------------------------------ units, pages and copies
         // Block c's range starts at c / n_blocks of the total cost; a cut within a sixteenth of a range of a unit's end moves there.
@@ -245,10 +260,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             else if (tiles - p.tile < snap) p.tile = tiles;
             return p;
         };
-        Place at = place_of(blockIdx.x);
-        const Place end = place_of(blockIdx.x + 1);
+        Place at = {}, end = {};
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) at = end, end = place_of(blockIdx.x + i);
         __syncwarp();  // the scan's place is the copies' from here on
-        uint32_t n_raw = 0, n_unit = 0;
         bool ok = true;
         int header[2] = {0, 0};  // of the block's two parts: 1 there, 2 the unit's last
         int4 header_unit = make_int4(0, 0, 0, 0);
@@ -297,6 +312,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     scales_of(quad, pid_next, sk_next, sv_next);
                     int tainted = INT32_MAX, ref = INT32_MIN, top = INT32_MIN, turn = 0;
                     const float f0 = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 0.f;
+                    float4 mine = make_float4(0.f, 0.f, 0.f, 0.f);  // of the lane's 16 keys: factor, log2(s_v / r), r / s_v, place
+                    bool even = false;                              // the scales of the four tiles are near enough for one reference
+                    // the reference for scales of V of which `most` is the largest; true: whatever is below it, down to nothing, is taken with it
+                    auto move_ref = [&](float most, bool fall) {
+                        if (most == 0.f) return true;
+                        const int e = min(static_cast<int>(__float_as_uint(most) >> 23) - 126, 127);  // most <= 2^e
+                        bool all = false;
+                        if (ref == INT32_MIN || e > ref) ref = e;
+                        else if (fall || e <= ref - kSpread) ref = max(e, top - kMostFall), all = ref > e;
+                        top = max(top, ref);
+                        return all;
+                    };
+                    auto inverse_ref = [&]() { return ref == INT32_MIN ? 1.f : (ref == 127 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(127 - ref) << 23)); };
+                    uint32_t place = kNoKeys;
+                    auto of_group = [&](float k, float v, float rel) {
+                        return make_float4(fmaxf(f0 * k, 0x1p-149f), v == 0.f ? 0.f : __log2f(rel), v == 0.f ? 1.f : __frcp_rn(rel), __uint_as_float(place));
+                    };
                     --quad;
                     for (int j = t0; j < t1 && ok; ++j) {
                         if ((j >> 2) != quad) {
@@ -306,80 +338,59 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                             good = key < key_end && pid >= 0 && pid < a.n_pages;
                             // what reads as NaN makes the rows that see it NaN, and nothing else
                             const bool bad = good && !(fabsf(sk) <= 3.402823466e38f && fabsf(sv) <= 3.402823466e38f);
-                            tainted = min(tainted, __reduce_min_sync(0xffffffffu, bad ? key & ~(page - 1) : INT32_MAX));
+                            if (__any_sync(0xffffffffu, bad)) tainted = min(tainted, __reduce_min_sync(0xffffffffu, bad ? key & ~(page - 1) : INT32_MAX));
                             if (bad) sk = sv = 0.f;
                             if (!(sk >= kSmallestScale)) sk = 0.f;
                             if (!(sv >= kSmallestScale)) sv = 0.f;
+                            place = good ? static_cast<uint32_t>((pid * a.kv_heads + kvh) << (a.page_log2 - 4)) + ((lane * 16 & (page - 1)) >> 4) : kNoKeys;
+                            if (good && sv == 0.f) place |= kZeroValues;
+                            // positive numbers order like their bits
+                            const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv)));
+                            const float least_v = __uint_as_float(__reduce_min_sync(0xffffffffu, sv == 0.f ? 0x7f800000u : __float_as_uint(sv)));
+                            even = most <= least_v * (1 << (kSpread - 1)) || most == 0.f;
+                            if (even) {
+                                // the reference stays where all scales of the quad are in its range
+                                const float now = inverse_ref();
+                                const bool fall = least_v * now < 1.f / (1 << kSpread);
+                                if (ref == INT32_MIN || most * now > 1.f || fall) even = !move_ref(most, fall) || most == 0.f;
+                                mine = of_group(sk, sv, sv * inverse_ref());
+                            }
                             pid_next = page_of(quad + 1);
                         }
-                        if ((j & 3) == 2 || j == t0) scales_of(quad + 1, pid_next, sk_next, sv_next);
-                        const int src = (j & 3) * 8 + (lane & 7), key0 = j * kTile;
-                        const float gk = __shfl_sync(0xffffffffu, sk, src), gv = __shfl_sync(0xffffffffu, sv, src);
+                        const int key0 = j * kTile;
                         unsigned todo = 0xffu;  // groups of keys that are still to be taken
                         while (todo && ok) {
-                            float most = (todo >> (lane & 7)) & 1u ? gv : 0.f;
-#pragma unroll
-                            for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-                            bool all = most == 0.f;
-                            if (!all) {
-                                const int e = min(static_cast<int>(__float_as_uint(most) >> 23) - 126, 127);  // most <= 2^e
-                                if (ref == INT32_MIN || e > ref) ref = e;
-                                else if (e <= ref - kSpread) {
-                                    ref = max(e, top - kMostFall);
-                                    all = ref > e;
-                                }
-                                top = max(top, ref);
+                            float4 entry = mine;
+                            const bool holds = (lane >> 3) == (j & 3);  // the lane knows a group of the tile
+                            if (even) {
+                                todo = 0;
+                            } else {
+                                const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, holds && (todo >> (lane & 7)) & 1u ? __float_as_uint(sv) : 0u));
+                                const bool all = move_ref(most, false);
+                                const float rel = sv * inverse_ref();
+                                const bool now = holds && (todo >> (lane & 7)) & 1u && (all || sv == 0.f || rel >= 1.f / (1 << kSpread));
+                                entry = of_group(sk, sv, rel);
+                                if (!now) entry.y = -INFINITY, entry.z = 0.f;
+                                todo &= ~((__ballot_sync(0xffffffffu, now) >> (8 * (j & 3))) & 0xffu);
                             }
-                            const float r = ref == INT32_MIN ? 1.f : __uint_as_float(static_cast<uint32_t>(127 + ref) << 23), inv_r = ref == 127 ? 0x1p-127f : 1.f / r;
-                            const float rel = gv * inv_r;
-                            const bool mine = ((todo >> (lane & 7)) & 1u) && (all || gv == 0.f || rel >= 1.f / (1 << kSpread));
-                            const unsigned sel = __ballot_sync(0xffffffffu, mine) & 0xffu;
-                            todo &= ~sel;
-                            const unsigned zero = __ballot_sync(0xffffffffu, gv == 0.f) & 0xffu;
                             int flags = by_keys ? kByKeys | (turn & 1 ? kSlot1 : kSlot0) : kSlot1 | (key0 <= last0 ? kSlot0 : 0);
                             ++turn;
                             const uint32_t ss = n_step % kSteps, sr = n_step / kSteps;
                             if (sr > 0 && !(ok = wait_warp(bar.step_empty + ss, sr - 1, 51))) break;
                             Step &st = steps[ss];
-                            if (lane < 8) {
-                                const float lv = !mine ? -INFINITY : (gv == 0.f ? 0.f : log2f(rel));
-                                st.group[lane] = make_float4(fmaxf(f0 * gk, 0x1p-149f), lv, !mine ? 0.f : (gv == 0.f ? 1.f : 1.f / rel), 0.f);
-                            } else if (lane == 8) {
-                                st.flags = flags, st.key0 = key0, st.limit = limit, st.ref = ref == INT32_MIN ? 0 : ref;
-                                st.token = token, st.n_tokens = n_tok, st.head = head, st.n_heads = n_heads;
-                                st.part = part, st.tainted = tainted, st.zero = static_cast<int>(zero);
+                            if (holds) {
+                                st.factor[lane & 7] = make_float4(entry.x, entry.x, entry.y, entry.y);
+                                st.weight[lane & 7] = entry.z, st.place[lane & 7] = __float_as_uint(entry.w);
+                            }
+                            if (lane == 0) {
+                                *reinterpret_cast<int4 *>(&st.flags) = make_int4(flags, key0, limit, ref == INT32_MIN ? 0 : ref);
+                                *reinterpret_cast<int4 *>(&st.token) = make_int4(token, n_tok, head, n_heads);
                             }
                             __syncwarp();
                             if (lane == 0) mbar_arrive(bar.step_full + ss);
                             ++n_step;
-                            // the pages' codes: each page by the lane that knows its first keys
-                            const int my_tile = quad * 4 + (lane >> 3), my_key = quad * (4 * kTile) + lane * 16;
-                            const bool copies = my_tile == j && good && (my_key & (page - 1)) == 0;
-                            const uint32_t bytes = static_cast<uint32_t>(page) * D;
-                            const uint32_t all_bytes = __popc(__ballot_sync(0xffffffffu, copies)) * bytes;
-                            const int64_t from = ((pid * a.kv_heads + kvh) << a.page_log2) * D;
-#pragma unroll 1
-                            for (int kv = 0; kv < 2 && ok; ++kv, ++n_raw) {
-                                const uint32_t rs = n_raw % kRaw, rr = n_raw / kRaw;
-                                if (rr > 0 && !(ok = wait_warp(bar.raw_empty + rs, rr - 1, 52))) break;
-                                if (lane == 0) mbar_arrive_expect_tx(bar.raw_full + rs, all_bytes);
-                                __syncwarp();
-                                if (copies) bulk_load_1d(smem + L::kRawRing + rs * L::kRawBytes + (lane & 7) * 16 * D, a.pages[kv].codes + from, bytes, bar.raw_full + rs);
-                            }
-                            if (ok && turn == 1) {  // behind the unit's first keys
-                                if (n_unit > 0 && !(ok = wait_warp(&bar.q_empty, n_unit - 1, 53))) break;
-                                if (lane == 0) {
-                                    const int slots = by_keys ? 1 : 2;
-                                    mbar_arrive_expect_tx(&bar.q_full, slots * kPieces * slot_tokens * heads * 128);
-                                    for (int i = 0; i < slots; ++i)
-#pragma unroll
-                                        for (int p = 0; p < kPieces; ++p)
-                                            tma_load_3d(&map_q, &bar.q_full, smem + L::kQ + i * L::kTileBytes + p * kPieceBytes, p * 64, head, token + i * slot_tokens);
-                                }
-                                __syncwarp();
-                                ++n_unit;
-                            }
                         }
+                        if ((j & 3) == 2 || (j == t0 && (j & 3) == 3)) scales_of(quad + 1, pid_next, sk_next, sv_next);
                     }
                     if (!ok) break;
                     const uint32_t ss = n_step % kSteps, sr = n_step / kSteps;
@@ -413,6 +424,60 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             a.headers[blockIdx.x * 4] = make_int4(header[0], header[1], slot_tokens, heads);
             a.headers[blockIdx.x * 4 + 1] = header_unit;
         }
+        } else if (warp == 11) {
+        // ------------------------------------------------------------ copies: keys of a step, values of the one before, queries of a unit
+        uint32_t n_unit = 0, n_raw = 0, place_v = kNoKeys;
+        bool ok = true, fresh = true, first = true;
+        const uint32_t bytes = static_cast<uint32_t>(page) * D;
+        const bool starts = lane < 8 && ((lane * 16) & (page - 1)) == 0;  // the lane's 16 keys are the first ones of a page
+        auto copy = [&](int kv, uint32_t place) {
+            const uint32_t rs = n_raw % kRaw, rr = n_raw / kRaw;
+            if (rr > 0 && !(ok = wait_warp(bar.raw_empty + rs, rr - 1, 52))) return;
+            ++n_raw;
+            const bool there = place != kNoKeys, zeros = there && kv == 1 && (place & kZeroValues);  // a page of V that stands for zeros, whatever its codes are
+            unsigned char *to = smem + L::kRawRing + rs * L::kRawBytes + lane * 16 * D;
+            const bool copies = there && starts && !zeros;
+            const unsigned who = __ballot_sync(0xffffffffu, copies);
+            if (__any_sync(0xffffffffu, zeros)) {
+                if (zeros)
+                    for (int i = 0; i < D; ++i) reinterpret_cast<uint4 *>(to)[i] = make_uint4(0, 0, 0, 0);
+                fence_proxy_async_smem();
+                __syncwarp();
+            }
+            if (lane == 0) mbar_arrive_expect_tx(bar.raw_full + rs, __popc(who) * bytes);
+            __syncwarp();
+            if (copies) bulk_load_1d(to, a.pages[kv].codes + static_cast<int64_t>(place & ~kZeroValues) * (16 * D), bytes, bar.raw_full + rs);
+        };
+        while (ok && next_step()) {
+            const Step &st = steps[n_step % kSteps];
+            const int flags = __shfl_sync(0xffffffffu, st.flags, 0), token = st.token, head = st.head;
+            const uint32_t place = lane < 8 ? st.place[lane] : kNoKeys;
+            done_step();
+            if (flags & kEnd) {
+                fresh = true;
+                continue;
+            }
+            // one loop for both, so that the code for a copy is there once
+#pragma unroll 1
+            for (int kv = flags & kExit ? 1 : 0; kv < (first ? 1 : 2) && ok; ++kv) copy(kv, kv == 0 ? place : place_v);
+            if (flags & kExit) break;
+            first = false, place_v = place;
+            if (ok && fresh) {
+                fresh = false;
+                if (n_unit > 0 && !(ok = wait_warp(&bar.q_empty, n_unit - 1, 53))) break;
+                ++n_unit;
+                if (lane == 0) {
+                    const int slots = flags & kByKeys ? 1 : 2;
+                    mbar_arrive_expect_tx(&bar.q_full, slots * kPieces * slot_tokens * heads * 128);
+#pragma unroll 1
+                    for (int i = 0; i < slots; ++i)
+#pragma unroll
+                        for (int p = 0; p < kPieces; ++p)
+                            tma_load_3d(&map_q, &bar.q_full, smem + L::kQ + i * L::kTileBytes + p * kPieceBytes, p * 64, head, token + i * slot_tokens);
+                }
+                __syncwarp();
+            }
+        }
         } else if (warp == 9) {
         // ------------------------------------------------------------ S = Q K^T
         const uint32_t idesc = kIdescBase<BF16> | (a.scale < 0.f ? 1u << 13 : 0u) | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);  // bit 13: A negated
@@ -430,8 +495,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             }
             if (fresh && !(ok = wait_warp(&bar.q_full, n_unit, 55))) break;
             fresh = false;
-            const uint32_t st = it % kStages;
-            if (!(ok = wait_warp(bar.kv_full + st, it / kStages, 54))) break;
+            const uint32_t at = it > 0 ? it - 1 : 0, st = at % kStages;
+            if (!(ok = wait_warp(bar.kv_full + st, at / kStages, 54))) break;
             const uint32_t k = k_desc + st * (L::kTileBytes >> 4);
 #pragma unroll 1  // the instructions of the roles that run together have to fit into the caches for them
             for (int s = 0; s < 2; ++s) {
@@ -440,11 +505,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 ++n_s;
                 tcgen05_fence_after();
                 const uint32_t q = q_desc + (flags & kByKeys ? 0 : s) * (L::kTileBytes >> 4);
-                if (elect_one())
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t off = ((kk / 4) * kPieceBytes + (kk % 4) * 32) >> 4;
-                    mma_smem_a(tmem + kColS, make_desc(q + off), make_desc(k + off), idesc, kk > 0);
+                if (elect_one()) {
+                    uint32_t off = 0;
+#pragma unroll 1
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        mma_smem_a(tmem + kColS, make_desc(q + off), make_desc(k + off), idesc, kk > 0);
+                        off += kk == 3 ? (kPieceBytes - 96) >> 4 : 32 >> 4;
+                    }
                 }
                 commit_elected(bar.s_full + s);
             }
@@ -455,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         // ------------------------------------------------------------ O += P V, in binary16
         constexpr uint32_t kIdesc = kIdescBase<false> | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
         const uint32_t v_desc = desc_lower(smem + L::kRing, kPieceBytes);
-        uint32_t it = 1, n_unit = 0, phase_p = 0, fresh = 3;  // bit s: slot s
+        uint32_t it = 2, n_unit = 0, phase_p = 0, fresh = 3;  // bit s: slot s
         bool ok = true;
         while (ok && next_step()) {
             const int flags = __shfl_sync(0xffffffffu, steps[n_step % kSteps].flags, 0);
@@ -481,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     tcgen05_fence_after();
                     const uint32_t v_half = v + half * (4 * 2048 >> 4), p_half = tmem + kColP + s * 64 + half * 32;
                     if (elect_one())
-#pragma unroll
+#pragma unroll 1
                     for (int kk = 0; kk < 4; ++kk)
                         tcgen05_mma_f16_tmem_a(tmem + kColO + s * 128, p_half + kk * 8, make_desc(v_half + kk * (2048 >> 4)), kIdesc, first && half + kk == 0 ? 0u : 1u);
                 }
@@ -494,61 +561,71 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         }
         }
     } else if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // ------------------------------------------------------------ codes to 16-bit operands in rows of 128 bytes with the 128-byte swizzle
+        // Keys of a step, then values of the one before: K0 K1 V0 K2 V1 ..  So a step's keys are there before the values of the step
+        // before have been asked for, and their place in the ring is that of values three steps back.
         const int t = threadIdx.x - 12 * 32;
-        uint32_t it = 0;
-        bool ok = true;
         constexpr int kPer = D / 8, kRows = 128 / kPer;  // threads of a token, tokens side by side
         const int row0 = t / kPer, c = t % kPer;
-        unsigned char *to0 = smem + L::kRing + (c / 8) * kPieceBytes + row0 * 128;
+        const uint32_t to0 = smem_u32(smem + L::kRing + (c / 8) * kPieceBytes + row0 * 128 + (((c & 7) ^ (row0 & 7)) << 4));
+        uint32_t n_raw = 0, n_k = 0;  // items so far, keys among them
+        bool ok = true;
         while (ok && next_step()) {
-            const int flags = steps[n_step % kSteps].flags, zero = steps[n_step % kSteps].zero;
+            const int flags = steps[n_step % kSteps].flags;
             done_step();
-            if (flags & kExit) break;
             if (flags & kEnd) continue;
+            if ((flags & kExit) && n_k == 0) break;
 #pragma unroll 1
-            for (int kv = 0; kv < 2; ++kv, ++it) {
-                const uint32_t rs = it % kRaw, st = it % kStages;
-                if (!(ok = wait_warp(bar.raw_full + rs, it / kRaw, 59))) break;
-                if (it >= kStages && !(ok = wait_warp(bar.kv_empty + st, it / kStages - 1, 65))) break;
-                const unsigned char *from = smem + L::kRawRing + rs * L::kRawBytes + t * 8;
-                unsigned char *to = to0 + st * L::kTileBytes;
-                if (!BF16 || kv == 1) {
-#pragma unroll 8
-                    for (int i = 0; i < kTile / kRows; ++i) {
-                        // byte c ^ 0x80 under the upper byte 0x64 is 1024 + (c + 128), less 1152, exactly c
-                        const uint2 x = *reinterpret_cast<const uint2 *>(from + i * kRows * D);
-                        const uint32_t keep = kv == 1 && (zero >> (i * kRows / 16)) & 1 ? 0u : 0xffffffffu;
-                        const uint32_t w0 = (x.x & keep) ^ 0x80808080u, w1 = (x.y & keep) ^ 0x80808080u;
-                        const int row = row0 + i * kRows;
-                        *reinterpret_cast<uint4 *>(to + i * kRows * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-                            make_uint4(hadd2_u32(prmt(w0, 0x64646464u, 0x4140), 0xE480E480u), hadd2_u32(prmt(w0, 0x64646464u, 0x4342), 0xE480E480u),
-                                       hadd2_u32(prmt(w1, 0x64646464u, 0x4140), 0xE480E480u), hadd2_u32(prmt(w1, 0x64646464u, 0x4342), 0xE480E480u));
+            for (int kv = flags & kExit ? 1 : 0; kv < (n_k == 0 ? 1 : 2); ++kv, ++n_raw) {
+                const uint32_t at = kv == 0 ? max(2 * n_k, 1u) - 1 : 2 * n_k;  // n_k: with kv = 1 the step is not counted yet
+                const uint32_t rs = n_raw % kRaw, st = at % kStages;
+                if (!(ok = wait_warp(bar.raw_full + rs, n_raw / kRaw, 59))) break;
+                if (at >= kStages && !(ok = wait_warp(bar.kv_empty + st, at / kStages - 1, 65))) break;
+                uint32_t from = smem_u32(smem + L::kRawRing + rs * L::kRawBytes + t * 8);
+                uint32_t to = to0 + st * L::kTileBytes;  // a thread's rows are a multiple of 8 apart: the swizzle is the same for all
+                // Short loops, whose instructions stay next to the scheduler: unrolled eight times this took three times as long, most of it
+                // waiting for instructions.  Loads are ahead of the stores, which the compiler would not let them pass.
+                auto convert = [&](auto codes4) {
+                    uint2 x = lds64(from), y = lds64(from + kRows * D);
+#pragma unroll 1
+                    for (int i = 0; i < kTile / kRows; i += 2) {
+                        from += 2 * kRows * D;
+                        const uint2 w0 = x, w1 = y;
+                        if (i + 2 < kTile / kRows) x = lds64(from), y = lds64(from + kRows * D);
+                        uint2 lo = codes4(w0.x), hi = codes4(w0.y);
+                        sts128(to, make_uint4(lo.x, lo.y, hi.x, hi.y));
+                        lo = codes4(w1.x), hi = codes4(w1.y);
+                        sts128(to + kRows * 128, make_uint4(lo.x, lo.y, hi.x, hi.y));
+                        to += 2 * kRows * 128;
                     }
+                };
+                if (!BF16 || kv == 1) {
+                    // byte c ^ 0x80 under the upper byte 0x64 is 1024 + (c + 128), less 1152, exactly c
+                    convert([](uint32_t w) {
+                        w ^= 0x80808080u;
+                        return make_uint2(hadd2_u32(prmt(w, 0x64646464u, 0x4140), 0xE480E480u), hadd2_u32(prmt(w, 0x64646464u, 0x4342), 0xE480E480u));
+                    });
                 } else {
-#pragma unroll 8
-                    for (int i = 0; i < kTile / kRows; ++i) {
-                        // under the upper byte 0x43 the lower seven bits are 128 + those bits, and the sign bit alone is 128 or 256: their difference is c
-                        const uint2 x = *reinterpret_cast<const uint2 *>(from + i * kRows * D);
-                        auto code2 = [](uint32_t w) {
+                    // under the upper byte 0x43 the lower seven bits are 128 + those bits, and the sign bit alone is 128 or 256: their difference is c
+                    convert([](uint32_t w) {
+                        auto code2 = [](uint32_t v) {
                             uint32_t d;
-                            asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(w & 0xff80ff80u), "r"(0xBF80BF80u), "r"(w & 0xff7fff7fu));
+                            asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(v & 0xff80ff80u), "r"(0xBF80BF80u), "r"(v & 0xff7fff7fu));
                             return d;
                         };
-                        const int row = row0 + i * kRows;
-                        *reinterpret_cast<uint4 *>(to + i * kRows * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-                            make_uint4(code2(prmt(x.x, 0x43434343u, 0x4140)), code2(prmt(x.x, 0x43434343u, 0x4342)),
-                                       code2(prmt(x.y, 0x43434343u, 0x4140)), code2(prmt(x.y, 0x43434343u, 0x4342)));
-                    }
+                        return make_uint2(code2(prmt(w, 0x43434343u, 0x4140)), code2(prmt(w, 0x43434343u, 0x4342)));
+                    });
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar.raw_empty + rs), mbar_arrive(bar.kv_full + st);
             }
+            ++n_k;
+            if (flags & kExit) break;
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         // ------------------------------------------------------------ softmax and output: a thread owns one row of a slot
         const int s = warp >> 2, row = (warp & 3) * 32 + lane;
         const int my_token = row / heads, my_head = row - my_token * heads;
@@ -711,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 float top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[15]));
 #pragma unroll
                 for (int k = 1; k < 15; k += 2) top = max3(top, __uint_as_float(w[k]), __uint_as_float(w[k + 1]));
-                best = fmaxf(best, top * st.group[g].x);
+                best = fmaxf(best, top * st.factor[g].x);
             }
             const int new_ref = st.ref;
             if (__any_sync(0xffffffffu, best - m > kMaxLead) || new_ref != ref) {
@@ -742,14 +819,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) x[c][k] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(x[c][k]), st.group[2 * c + k / 16].x), base));
+                    for (int k = 0; k < 32; ++k) x[c][k] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(x[c][k]), st.factor[2 * c + k / 16].x), base));
             }
             auto quarter = [&](int c, uint32_t *p) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float4 g = st.group[2 * c + h];
-                    const float f1 = far ? 1.f : g.x, s1 = sub1 + g.y;
-                    const float2 ff = make_float2(f1, f1), sub = make_float2(s1, s1);
+                    const float4 g = st.factor[2 * c + h];
+                    const float weight = st.weight[2 * c + h];
+                    const float2 ff = far ? make_float2(1.f, 1.f) : make_float2(g.x, g.y), sub = add2(make_float2(sub1, sub1), make_float2(g.z, g.w));
                     float2 part = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -758,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                         part = add2(part, e);
                         p[8 * h + k] = Elem<false>::from_float2(e.x, e.y);
                     }
-                    l = fma2(part, make_float2(g.z, g.z), l);
+                    l = fma2(part, make_float2(weight, weight), l);
                 }
             };
             auto hand_over = [&](int half) {
