@@ -519,15 +519,16 @@ pd_status pd_kv_append_rope_bf16(const void *q, int64_t q_token_stride, int64_t 
  *
  *   q   : in,  [n_tokens, q_heads, head_dim], packed by cu_seqlens: the last cu_seqlens[b + 1] - cu_seqlens[b] tokens of sequence b,
  *         which has seq_lens[b] in all; none, one or many
- *   max_new : the most new tokens of a sequence, 0 for not known
+ *   max_new : the most new tokens of a sequence, 0 for not known: where at most 16 pairs of a token and a query head share a key/value head,
+ *         max_new * (q_heads / kv_heads), a call that says so is quicker
  *   out : out, [n_tokens, q_heads, head_dim]: token i of the n new ones attends to the cached tokens 0 .. seq_lens[b] - n + i
  * Rows of n_tokens that no sequence claims are left as they are.  Slots of a page behind what a token attends to and pages that it does not
  * reach have no influence on it, whatever they hold; a page whose scale is not finite makes the tokens that attend to any of it NaN.
  * Weights are rounded to binary16 (relative to the largest, times the scale of V's page, times 2^7) for their product with V; pages whose scale of V is below 2^-67 of the
  * largest of the sequence lose precision.  Offsets that decrease, more new tokens than max_new or than seq_lens[b] and lengths beyond the table
  * latch PD_ERR_BAD_INDEX, and the sequence is left out.  The same call gives the same bits.
- * Workspace: pd_workspace_bytes(PD_OP_ATTN_CHUNK, 0, 0, 0, 0) bytes (about 40 MB, for parts of rows whose keys are dealt to several blocks), of
- * which only the status words have to be zero before the first call.
+ * Workspace: pd_workspace_bytes(PD_OP_ATTN_CHUNK, 0, 0, 0, 0) bytes (about 42 MB, for parts of rows whose keys are dealt to several blocks), of
+ * which the first 131072 have to be zero before the first call.
  */
 pd_status pd_attn_chunk(const void *q, int64_t q_token_stride, int64_t q_head_stride, const int32_t *cu_seqlens, int32_t n_seqs, int64_t n_tokens,
                         int64_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale, const int8_t *k_codes,

@@ -388,9 +388,9 @@ def _attn_workspace(index: int, stream: int, op: int = OP_ATTN):
     cache = (_chunk_graph_ws if capture else _chunk_ws_cache) if op == OP_ATTN_CHUNK else (_attn_graph_ws if capture else _attn_ws_cache)
     ws = cache.get((index, stream))
     if ws is None or ws[3] != capture:
-        if op == OP_ATTN_CHUNK:  # of which only the status words have to be zero
+        if op == OP_ATTN_CHUNK:  # of which only the beginning has to be zero
             t = torch.empty(workspace_bytes(op), dtype=torch.uint8, device=torch.device("cuda", index))
-            t[:256].zero_()
+            t[:1 << 17].zero_()
         else:
             t = torch.zeros(workspace_bytes(op), dtype=torch.uint8, device=torch.device("cuda", index))
         ws = cache[index, stream] = (t, t.data_ptr(), t.numel(), capture)

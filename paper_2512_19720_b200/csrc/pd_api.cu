@@ -174,7 +174,7 @@ size_t pd_workspace_bytes(int op, int64_t M, int32_t V, int64_t d_out, int64_t d
         case PD_OP_ATTN:
             return kStatusBytes + attn_cache_scratch_bytes();
         case PD_OP_ATTN_CHUNK:
-            return kStatusBytes + attn_chunk_scratch_bytes();
+            return kStatusBytes + attn_cache_scratch_bytes() + attn_chunk_scratch_bytes();
         case PD_OP_FIT_LAYER:
             return M > 0 ? kStatusBytes + fit_layer_scratch_bytes(M, M, d_out, d_in) : 0;
         case PD_OP_MERGE:

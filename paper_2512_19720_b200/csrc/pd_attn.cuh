@@ -49,6 +49,9 @@ struct CacheAttnArgs {
     uint32_t *status;
     unsigned int *counters;  // zero on entry, zero again on return
     float *partial;
+    // several new tokens a sequence
+    const int32_t *cu_seqlens;
+    int n_tokens, max_new;
 };
 
 // Rotary positions: pair i of a head turns by positions[axes[i]][token] * inv_freq[i].
@@ -98,5 +101,8 @@ pd_status launch_rope(const RopeArgs &a, bool interleaved, bool bf16, cudaStream
 pd_status launch_kv_append_rope(const AppendRopeArgs &a, bool interleaved, bool bf16, cudaStream_t stream);
 pd_status launch_attn_chunk(ChunkArgs a, unsigned char *scratch, bool bf16, cudaStream_t stream);
 pd_status launch_attn_cache(CacheAttnArgs a, unsigned char *scratch, bool bf16, cudaStream_t stream);
+// The same for max_new tokens a sequence; max_new * (q_heads / kv_heads) is at most kCacheRows.
+constexpr int kCacheRows = 16;
+pd_status launch_attn_cache_rows(CacheAttnArgs a, unsigned char *scratch, bool bf16, cudaStream_t stream);
 
 }  // namespace pd

@@ -99,13 +99,28 @@ constexpr int kSegmentCost = 2;
 constexpr int kMinUnits = 2;
 __device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + kTile - 1) / kTile : 1; }
 
+// Several new tokens a sequence (CHUNK): a segment's rows are tokens and, of each, the heads that share the key/value head, heads first;
+// the first tokens do not attend to the last keys.  Up to 16 rows; the sequences' tokens are packed.
+template <bool CHUNK>
+struct Rows {
+    const CacheAttnArgs &a;
+    int group;
+    __device__ __forceinline__ int first(int b) const { return CHUNK ? __ldg(a.cu_seqlens + b) : b; }
+    __device__ __forceinline__ int tokens(int b) const { return CHUNK ? __ldg(a.cu_seqlens + b + 1) - __ldg(a.cu_seqlens + b) : 1; }
+    // where a row's values start in a tensor of tokens; head0: the segment's first head
+    __device__ __forceinline__ int64_t at(const HeadsView &v, int token0, int head0, int r) const {
+        const int t = CHUNK ? r / group : 0;
+        return static_cast<int64_t>(token0 + t) * v.token_stride + static_cast<int64_t>(head0 + r - t * group) * v.head_stride;
+    }
+};
+
 // A partial result of a segment in a warp's shared memory: which one, and where it starts in the order of all tiles.
 struct Piece {
     int first;  // the unit of the segment's first tile; -1: none
-    int tiles, b, head0, rows;
+    int tiles, token, head0, rows;  // token: the first row of q and out
 };
 
-template <int D, int NT, bool BF16>
+template <int D, int NT, bool BF16, bool CHUNK>
 __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_kernel(const CacheAttnArgs a) {
     using E = Elem<BF16>;
     using L = CacheShape<D, NT>;
@@ -124,13 +139,21 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const int group = a.q_heads / a.kv_heads;
-    const int chunks = (group + L::kRows - 1) / L::kRows;
+    const int chunks = CHUNK ? 1 : (group + L::kRows - 1) / L::kRows;
+    const Rows<CHUNK> row_of = {a, group};
     const int per_seq = a.kv_heads * chunks;  // segments of a sequence
     const int page = 1 << a.page_log2;
     const int64_t room = static_cast<int64_t>(a.table_width) << a.page_log2;
 
+    auto in_range = [&](int b) {  // what is not is reported; pieces are left out then
+        const int n = __ldg(a.seq_lens + b);
+        if (!CHUNK) return n >= 0 && n <= room;
+        const int first = __ldg(a.cu_seqlens + b), last = __ldg(a.cu_seqlens + b + 1);
+        return first >= 0 && last >= first && last <= a.n_tokens && last - first <= a.max_new && n >= last - first && n <= room;
+    };
     auto length = [&](int b) {
         const int n = __ldg(a.seq_lens + b);
+        if (CHUNK) return in_range(b) && row_of.tokens(b) > 0 ? n : 0;
         return n < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(n), room));
     };
 
@@ -140,8 +163,8 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     const int share = (a.n_seqs + kThreads - 1) / kThreads;
     int sum = 0, first_len = 0;
     for (int b = threadIdx.x * share; b < min(a.n_seqs, static_cast<int>(threadIdx.x + 1) * share); ++b) {
-        const int raw = __ldg(a.seq_lens + b), n = length(b);
-        if (blockIdx.x == 0 && raw != n) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
+        const int n = length(b);
+        if (blockIdx.x == 0 && !in_range(b)) latch_error(a.status, PD_ERR_BAD_INDEX, static_cast<uint32_t>(b));
         if (b == static_cast<int>(threadIdx.x) * share) first_len = n;
         sum += tiles_of(n) + kSegmentCost;
     }
@@ -203,7 +226,8 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         const int n_tiles = tiles_of(len), first_unit = at - i0;
         const int kvh = s / chunks, chunk = s - kvh * chunks;
         const int head0 = kvh * group + chunk * L::kRows;
-        const int rows = min(L::kRows, group - chunk * L::kRows);
+        const int new_tokens = CHUNK && len > 0 ? row_of.tokens(b) : 0, token0 = CHUNK && len > 0 ? row_of.first(b) : b;
+        const int rows = CHUNK ? new_tokens * group : min(L::kRows, group - chunk * L::kRows);
         const int i1 = min(n_tiles, range1 - first_unit);
         i0 = max(i0, 0);
         if (i1 <= i0) break;  // of this segment only the units before its tiles
@@ -232,6 +256,8 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                                     pid[k] = p;
                                     sk[k] = a.pages[0].scale[p * a.kv_heads + kvh];
                                     sv[k] = a.pages[1].scale[p * a.kv_heads + kvh];
+                                    // some rows may attend to the page and others not: those that do get scores of NaN
+                                    if (CHUNK && !(fabsf(sk[k]) <= 3.402823466e38f && fabsf(sv[k]) <= 3.402823466e38f)) sk[k] = __int_as_float(0x7fc00000), sv[k] = 0.f;
                                 }
                             }
                         }
@@ -270,6 +296,11 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
         }
         float o[MT][NT][4];
         float m[NT][2], mu[NT][2], l[NT][2], qs[NT][2];
+        int hidden[NT][2];  // keys at the end that a row does not attend to
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) hidden[n][k] = CHUNK ? max(new_tokens - 1 - (n * 8 + 2 * t + k) / group, 0) : 0;
         uint32_t qf[KS][NT][3][2];
         float ref = 0.f, inv_ref = 0.f, ref_top = 0.f;  // the reference scale of V, its reciprocal, and the largest that O was summed with
 #pragma unroll
@@ -289,8 +320,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
             for (int c = 0; c < KC; ++c) {
                 uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
                 if (r < rows) {
-                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q.ptr) + b * a.q.token_stride +
-                                                                     (head0 + r) * a.q.head_stride + 16 * (t + 4 * c));
+                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q.ptr) + row_of.at(a.q, token0, head0, r) + 16 * (t + 4 * c));
                     w[0] = p[0], w[1] = p[1];
                 }
                 const uint32_t u[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
@@ -350,7 +380,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                 const float4 sc = meta[st];
                 if (half == 0 && fmaxf(sc.z, sc.w) > 8.f * fminf(sc.z, sc.w) && fminf(sc.z, sc.w) > 0.f) half = 1;
                 const int rest = static_cast<int>(min(len - static_cast<int64_t>(i) * kTile, static_cast<int64_t>(kTile)));  // tokens of the tile
-                const int end[2] = {half == 2 ? 0 : rest, half == 1 ? 0 : rest};
+                const int end[2] = {half == 2 ? 0 : rest, half == 1 ? 0 : rest}, left = len - i * kTile;
 
                 // S^T = K Q^T
                 float acc[2][NT][4];
@@ -395,7 +425,9 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const float f = (h == 0 ? sc.x : sc.y) * qs[n][k & 1];
-                            acc[h][n][k] = 16 * h + g + 8 * (k >> 1) < end[h] ? acc[h][n][k] * f : -INFINITY;
+                            const int key = 16 * h + g + 8 * (k >> 1);
+                            const bool seen = key < end[h] && (!CHUNK || key + hidden[n][k & 1] < left);
+                            acc[h][n][k] = seen ? acc[h][n][k] * f : -INFINITY;
                             lead |= acc[h][n][k] > __fadd_rd(m[n][k & 1], kMaxLead);  // rounded down: P's range is bounded for large scores too
                         }
                 const float sv[2] = {half == 2 ? 0.f : sc.z, half == 1 ? 0.f : sc.w}, sv_hi = fmaxf(sv[0], sv[1]);
@@ -513,8 +545,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                         uint32_t w[VB / 2];
 #pragma unroll
                         for (int j = 0; j < VB / 2; ++j) w[j] = E::from_float2(o[j][n][k] * f, o[j][n][k + 2] * f);
-                        uint4 *p = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + b * a.out.token_stride +
-                                                             (head0 + r) * a.out.head_stride + VB * g);
+                        uint4 *p = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + row_of.at(a.out, token0, head0, r) + VB * g);
 #pragma unroll
                         for (int j = 0; j < VB / 8; ++j) p[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
                     }
@@ -534,7 +565,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                             *reinterpret_cast<float2 *>(po + r * D + VB * g + 2 * j) = make_float2(o[j][n][k] * kPart * ref, o[j][n][k + 2] * kPart * ref);
                     }
                 }
-            if (lane == 0) pieces[warp][slot] = {first_unit, n_tiles, b, head0, rows};
+            if (lane == 0) pieces[warp][slot] = {first_unit, n_tiles, token0, head0, rows};
         }
         if (i1 < n_tiles) break;
         at = first_unit + n_tiles;
@@ -566,8 +597,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     };
     auto store_out = [&](const Piece &p, int r, const Sum &x) {
         const float f = x.l == 0.f ? 0.f : 1.f / kPart / x.l;
-        uint32_t *y = reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + p.b * a.out.token_stride +
-                                                   (p.head0 + r) * a.out.head_stride + V * lane);
+        uint32_t *y = reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + row_of.at(a.out, p.token, p.head0, r) + V * lane);
         if (V == 4) *reinterpret_cast<uint2 *>(y) = make_uint2(E::from_float2(x.o[0] * f, x.o[1] * f), E::from_float2(x.o[V - 2] * f, x.o[V - 1] * f));
         else *y = E::from_float2(x.o[0] * f, x.o[1] * f);
     };
@@ -675,11 +705,11 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
     }
 }
 
-template <int D, int NT, bool BF16>
+template <int D, int NT, bool BF16, bool CHUNK>
 pd_status launch(const CacheAttnArgs &a, int grid, cudaStream_t stream) {
     using L = CacheShape<D, NT>;
     static std::atomic<bool> done[kMaxDevices];
-    if (!ensure_dynamic_smem(attn_cache_kernel<D, NT, BF16>, L::kTotal, done)) return PD_ERR_CUDA;
+    if (!ensure_dynamic_smem(attn_cache_kernel<D, NT, BF16, CHUNK>, L::kTotal, done)) return PD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
     cfg.blockDim = dim3(L::kThreads);
@@ -691,7 +721,7 @@ pd_status launch(const CacheAttnArgs &a, int grid, cudaStream_t stream) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     count_launch();
-    return cuda_ok(cudaLaunchKernelEx(&cfg, attn_cache_kernel<D, NT, BF16>, a));
+    return cuda_ok(cudaLaunchKernelEx(&cfg, attn_cache_kernel<D, NT, BF16, CHUNK>, a));
 }
 
 }  // namespace
@@ -700,17 +730,25 @@ size_t attn_cache_scratch_bytes() {
     return kCounterBytes + static_cast<size_t>(min(sm_count(), kMaxGrid)) * 2 * max(CacheShape<128, 1>::kPiece, CacheShape<128, 2>::kPiece);
 }
 
-pd_status launch_attn_cache(CacheAttnArgs a, unsigned char *scratch, bool bf16, cudaStream_t stream) {
+template <bool CHUNK>
+pd_status launch_for(CacheAttnArgs a, unsigned char *scratch, int rows, bool bf16, cudaStream_t stream) {
     a.counters = reinterpret_cast<unsigned int *>(scratch);
     a.partial = reinterpret_cast<float *>(scratch + kCounterBytes);
     const int grid = min(sm_count(), kMaxGrid);
-    const bool wide = a.q_heads / a.kv_heads > 8;  // more than 8 heads share a key/value head: two products of 8 heads per load of the codes
+    const bool wide = rows > 8;  // more than 8 rows share a key/value head: two products of 8 rows per load of the codes
     if (a.head_dim == 128) {
-        if (wide) return bf16 ? launch<128, 2, true>(a, grid, stream) : launch<128, 2, false>(a, grid, stream);
-        return bf16 ? launch<128, 1, true>(a, grid, stream) : launch<128, 1, false>(a, grid, stream);
+        if (wide) return bf16 ? launch<128, 2, true, CHUNK>(a, grid, stream) : launch<128, 2, false, CHUNK>(a, grid, stream);
+        return bf16 ? launch<128, 1, true, CHUNK>(a, grid, stream) : launch<128, 1, false, CHUNK>(a, grid, stream);
     }
-    if (wide) return bf16 ? launch<64, 2, true>(a, grid, stream) : launch<64, 2, false>(a, grid, stream);
-    return bf16 ? launch<64, 1, true>(a, grid, stream) : launch<64, 1, false>(a, grid, stream);
+    if (wide) return bf16 ? launch<64, 2, true, CHUNK>(a, grid, stream) : launch<64, 2, false, CHUNK>(a, grid, stream);
+    return bf16 ? launch<64, 1, true, CHUNK>(a, grid, stream) : launch<64, 1, false, CHUNK>(a, grid, stream);
+}
+
+pd_status launch_attn_cache(CacheAttnArgs a, unsigned char *scratch, bool bf16, cudaStream_t stream) {
+    return launch_for<false>(a, scratch, a.q_heads / a.kv_heads, bf16, stream);
+}
+pd_status launch_attn_cache_rows(CacheAttnArgs a, unsigned char *scratch, bool bf16, cudaStream_t stream) {
+    return launch_for<true>(a, scratch, a.max_new * (a.q_heads / a.kv_heads), bf16, stream);
 }
 
 }  // namespace pd

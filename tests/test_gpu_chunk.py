@@ -98,9 +98,28 @@ def test_chunk_matches_the_definition(api, new, hq, hkv, d, page, dtype):
     held = [77, 0, 130, 1, 250][:len(new)]
     lens = [a + b for a, b in zip(held, new)]
     pages = Pages(lens, hkv, d, page, 5 + hq)
-    got = check(api, pages, queries(sum(new), hq, d, dtype, sum(new)), lens, new)
-    again = api.pd_attn_chunk(queries(sum(new), hq, d, dtype, sum(new)), *pages.tensors(), offsets(new), i32(lens), pages.block_table, max(new))
-    assert torch.equal(got, again)  # the same bits
+    q = queries(sum(new), hq, d, dtype, sum(new))
+    for most in (0, max(new)):  # few rows, where the most new tokens are known, go to another kernel
+        got = check(api, pages, q, lens, new, max_new=most)
+        again = api.pd_attn_chunk(q, *pages.tensors(), offsets(new), i32(lens), pages.block_table, most)
+        assert torch.equal(got, again)  # the same bits
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hq,hkv,d,page,most", [(4, 4, 128, 64, 8), (5, 5, 64, 16, 16), (16, 8, 128, 32, 4), (8, 2, 64, 128, 4), (32, 2, 128, 16, 1), (8, 1, 128, 64, 2), (12, 4, 64, 32, 5)])
+def test_chunk_few_rows(api, hq, hkv, d, page, most, dtype):
+    """At most 16 rows share a key/value head: every number of tokens, none among them, at the ends of pages and tiles, short and long."""
+    rng = np.random.default_rng(most)
+    new = list(range(most + 1)) + rng.integers(0, most + 1, 20).tolist() + [most, 1]
+    held = rng.choice([0, 1, 15, 16, 31, 32, 33, 64, 127, 128, 300], len(new)).tolist()
+    held[-2:] = [5000, 3000]
+    lens = [a + b for a, b in zip(held, new)]
+    pages = Pages(lens, hkv, d, page, 31 + most)
+    q = queries(sum(new), hq, d, dtype, 7)
+    got = check(api, pages, q, lens, new, max_new=most)
+    for _ in range(3):
+        assert torch.equal(got, api.pd_attn_chunk(q, *pages.tensors(), offsets(new), i32(lens), pages.block_table, most))
+    check(api, pages, q, lens, new, -0.1, max_new=most)
 
 
 @pytest.mark.parametrize("hq,hkv,d", [(8, 8, 128), (16, 2, 64), (16, 1, 128), (130, 1, 64), (300, 2, 64), (40, 8, 128)])
@@ -196,25 +215,28 @@ def test_chunk_every_scale_counts(api, order):
         assert seen.all()
 
 
-def test_chunk_what_is_not_attended_to_has_no_influence(api):
+@pytest.mark.parametrize("first,new,most", [(30, [70, 4], 0), (3, [8, 4], 8)])
+def test_chunk_what_is_not_attended_to_has_no_influence(api, first, new, most):
     """Codes and scales of later tokens, of slots behind the end, of pages that are not reached; pages that read as NaN."""
-    new, lens, page = [70, 4], [200, 75], 32
+    page, last = 32, new[0]
+    lens = [160 - first + last, 75]  # token 160 is new token `first`
     for dtype in TYPES:
         pages = Pages(lens, 2, 64, page, 59)
-        q = queries(74, 4, 64, dtype, 61)
-        run = lambda: api.pd_attn_chunk(q, *pages.tensors(), offsets(new), i32(lens), pages.block_table)  # noqa: E731
+        q = queries(sum(new), 4, 64, dtype, 61)
+        run = lambda: api.pd_attn_chunk(q, *pages.tensors(), offsets(new), i32(lens), pages.block_table, most)  # noqa: E731
         clean = run()
-        pages.codes[0][pages.table[0, 6], :, 200 - 6 * page:] = 77
-        pages.codes[1][pages.table[0, 6], :, 200 - 6 * page:] = -77
+        end = pages.table[0, lens[0] // page]
+        pages.codes[0][end, :, lens[0] % page:] = 77
+        pages.codes[1][end, :, lens[0] % page:] = -77
         assert torch.equal(run(), clean)
         for which in (0, 1):
             for bad in (float("nan"), float("inf")):
                 held = pages.scales[which][pages.table[0, 5], 1].clone()
-                pages.scales[which][pages.table[0, 5], 1] = bad  # tokens 160 .. 191, of which token 160 is new token 30
+                pages.scales[which][pages.table[0, 5], 1] = bad  # tokens 160 .. 191
                 got = run()
                 pages.scales[which][pages.table[0, 5], 1] = held
-                assert bool(torch.isnan(got[30:70, 2:].float()).all())
-                assert torch.equal(got[:30], clean[:30]) and torch.equal(got[:, :2], clean[:, :2]) and torch.equal(got[70:], clean[70:])
+                assert bool(torch.isnan(got[first:last, 2:].float()).all())
+                assert torch.equal(got[:first], clean[:first]) and torch.equal(got[:, :2], clean[:, :2]) and torch.equal(got[last:], clean[last:])
 
 
 def test_chunk_strides_and_untouched_rows(api):
@@ -234,22 +256,28 @@ def test_chunk_strides_and_untouched_rows(api):
     assert torch.equal(api.pd_attn_chunk(heads_first, *pages.tensors(), offsets(new), i32(lens), table[:, :pages.block_table.shape[1]]), want)
 
 
-def test_chunk_bad_indices_are_reported(api):
-    new, lens = [50, 4], [100, 40]
+@pytest.mark.parametrize("few", [False, True])
+def test_chunk_bad_indices_are_reported(api, few):
+    new, lens = ([50, 4], [100, 40]) if not few else ([6, 4], [100, 40])
+    a, b = new[0], sum(new)
     pages = Pages(lens, 2, 64, 32, 71)
-    q = queries(54, 4, 64, torch.float16, 73)
-    call = lambda cu, n, table, most=0: api.pd_attn_chunk(q, *pages.tensors(), i32(cu), i32(n), table, most)  # noqa: E731
+    q = queries(b, 4, 64, torch.float16, 73)
+    call = lambda cu, n, table, most=8 if few else 0: api.pd_attn_chunk(q, *pages.tensors(), i32(cu), i32(n), table, most)  # noqa: E731
     for entry in (-1, pages.codes[0].shape[0], 2 ** 31 - 1):
         table = pages.block_table.clone()
         table[0, 2] = entry
-        got = call([0, 50, 54], lens, table)
+        got = call([0, a, b], lens, table)
         assert api.pd_device_status(api.chunk_workspace()) == 8
-        check(api, pages, q, lens, new, got=got, only={50, 51, 52, 53})
-    for cu, n, most in (([0, 50, 54], [49, 40], 0), ([0, 50, 54], [pages.block_table.shape[1] * 32 + 1, 40], 0), ([0, 50, 54], [-5, 40], 0), ([0, 50, 54], lens, 49),
-                        ([0, 55, 54], lens, 0), ([-1, 50, 54], lens, 0)):
-        got = call(cu, n, pages.block_table.clamp(min=0), most)
-        assert api.pd_device_status(api.chunk_workspace()) == 8, (cu, n, most)
+        check(api, pages, q, lens, new, got=got, only=set(range(a, b)))
+    bad = [([0, a, b], [a - 1, 40]), ([0, a, b], [pages.block_table.shape[1] * 32 + 1, 40]), ([0, a, b], [-5, 40]), ([0, b + 1, b], lens), ([-1, a, b], lens), ([0, a, b], [0, 40])]
+    for cu, n in bad:
+        call(cu, n, pages.block_table.clamp(min=0))
+        assert api.pd_device_status(api.chunk_workspace()) == 8, (cu, n)
+    call([0, a, b], lens, pages.block_table, a - 1)
+    assert api.pd_device_status(api.chunk_workspace()) == 8
     assert api.pd_device_status(api.chunk_workspace()) == 0
+    none = call([0, 0, 0], lens, pages.block_table)  # no new tokens: nothing to say
+    assert none.shape == q.shape and api.pd_device_status(api.chunk_workspace()) == 0
     assert api.pd_attn_chunk(q[:0], *pages.tensors(), i32([0, 0, 0]), i32(lens), pages.block_table).shape == (0, 4, 64)
 
 
@@ -260,6 +288,7 @@ def test_chunk_agrees_with_single_tokens_and_prompts(api):
     q = queries(n, hq, d, torch.float16, 83)
     piece = check(api, pages, q, [n], [n])
     one = api.pd_attn_cache(q[-1:], *pages.tensors(), i32([n]), pages.block_table)
+    assert torch.equal(one, api.pd_attn_chunk(q[-1:], *pages.tensors(), offsets([1]), i32([n]), pages.block_table, 1))
     _, bound = definition(pages, f64(q), [n], [n], d ** -0.5, torch.float16, {n - 1})
     assert np.all(np.abs(f64(one[0]) - f64(piece[-1])) <= 2 * bound[-1])
 
