@@ -28,7 +28,7 @@ namespace {
 constexpr int kTile = 128;  // rows of a slot, keys of a tile
 constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
-constexpr int kSteps = 6;       // steps that the producer may be ahead
+constexpr int kSteps = 4;       // steps that the producer may be ahead
 constexpr int kReaders = 15;   // warps that read a step
 constexpr int kMaxGrid = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -102,11 +102,21 @@ __device__ __forceinline__ void sts128(uint32_t at, const uint4 &x) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
 }
 
-__device__ __forceinline__ uint32_t clock32() {
-    uint32_t t;
-    asm volatile("mov.u32 %0, %%clock;" : "=r"(t));
-    return t;
+__device__ __forceinline__ bool mbar_sleep_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000) : "memory");
+    return ok != 0;
 }
+
+// A place in a ring of N stages, and the parity of its round.
+template <uint32_t N>
+struct Ring {
+    uint32_t stage = 0, parity = 0;
+    __device__ __forceinline__ void forward(uint32_t n) {
+        stage += n;
+        if (stage >= N) stage -= N, parity ^= 1u;
+    }
+};
 
 // Units of a sequence's rows that read one key/value head (a *stream*), and what they cost.
 struct Stream {
@@ -146,16 +156,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
     const int per_seq = a.kv_heads * chunks;  // streams
     const int page = 1 << a.page_log2;
     const int64_t room = static_cast<int64_t>(a.table_width) << a.page_log2;
-    // Bounded; the first one to give up says where, and the block's last act is to report it.  Short, because it is in the code of every
-    // role many times over.
-    auto wait = [&](uint64_t *b, uint32_t parity, int where) {
-        const uint32_t since = clock32();
-        bool done;
-        while (!(done = mbar_try_wait(b, parity & 1u)) && clock32() - since <= static_cast<uint32_t>(kWaitCycles)) {}
-        if (!done) *abort_flag = where;
-        return done;
+    // Bounded: a question sleeps for up to 20 us, and there are 2^16 of them.  The first one to give up says where, and the block's last act
+    // is to report it.  Short, because it is in the code of every role many times over.  On a barrier that has not been used yet the
+    // phase before the first one counts as over, so that who waits for "the use before mine" need not know whether there was one.
+    auto wait_warp = [&](uint64_t *b, uint32_t parity, int where) {
+        int left = 1 << 16;
+#pragma unroll 1
+        while (!__all_sync(0xffffffffu, mbar_sleep_wait(smem_u32(b), parity & 1u)) && --left) {}
+        if (!left) *abort_flag = where;
+        return left != 0;
     };
-    auto wait_warp = [&](uint64_t *b, uint32_t parity, int where) { return __all_sync(0xffffffffu, wait(b, parity, where)) != 0; };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSteps; ++i) mbar_init(bar.step_full + i, 1), mbar_init(bar.step_empty + i, kReaders);
@@ -376,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                             int flags = by_keys ? kByKeys | (turn & 1 ? kSlot1 : kSlot0) : kSlot1 | (key0 <= last0 ? kSlot0 : 0);
                             ++turn;
                             const uint32_t ss = n_step % kSteps, sr = n_step / kSteps;
-                            if (sr > 0 && !(ok = wait_warp(bar.step_empty + ss, sr - 1, 51))) break;
+                            if (!(ok = wait_warp(bar.step_empty + ss, sr - 1, 51))) break;
                             Step &st = steps[ss];
                             if (holds) {
                                 st.factor[lane & 7] = make_float4(entry.x, entry.x, entry.y, entry.y);
@@ -394,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     }
                     if (!ok) break;
                     const uint32_t ss = n_step % kSteps, sr = n_step / kSteps;
-                    if (sr > 0 && !(ok = wait_warp(bar.step_empty + ss, sr - 1, 51))) break;
+                    if (!(ok = wait_warp(bar.step_empty + ss, sr - 1, 51))) break;
                     if (lane == 0) {
                         Step &st = steps[ss];
                         st.flags = kEnd | (by_keys ? kByKeys : 0), st.limit = limit, st.token = token, st.n_tokens = n_tok, st.head = head, st.n_heads = n_heads;
@@ -413,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         }
         if (ok) {
             const uint32_t ss = n_step % kSteps, sr = n_step / kSteps;
-            if (sr == 0 || wait_warp(bar.step_empty + ss, sr - 1, 51)) {
+            if (wait_warp(bar.step_empty + ss, sr - 1, 51)) {
                 if (lane == 0) {
                     steps[ss].flags = kExit;
                     mbar_arrive(bar.step_full + ss);
@@ -432,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         const bool starts = lane < 8 && ((lane * 16) & (page - 1)) == 0;  // the lane's 16 keys are the first ones of a page
         auto copy = [&](int kv, uint32_t place) {
             const uint32_t rs = n_raw % kRaw, rr = n_raw / kRaw;
-            if (rr > 0 && !(ok = wait_warp(bar.raw_empty + rs, rr - 1, 52))) return;
+            if (!(ok = wait_warp(bar.raw_empty + rs, rr - 1, 52))) return;
             ++n_raw;
             const bool there = place != kNoKeys, zeros = there && kv == 1 && (place & kZeroValues);  // a page of V that stands for zeros, whatever its codes are
             unsigned char *to = smem + L::kRawRing + rs * L::kRawBytes + lane * 16 * D;
@@ -464,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             first = false, place_v = place;
             if (ok && fresh) {
                 fresh = false;
-                if (n_unit > 0 && !(ok = wait_warp(&bar.q_empty, n_unit - 1, 53))) break;
+                if (!(ok = wait_warp(&bar.q_empty, n_unit - 1, 53))) break;
                 ++n_unit;
                 if (lane == 0) {
                     const int slots = flags & kByKeys ? 1 : 2;
@@ -482,8 +492,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         // ------------------------------------------------------------ S = Q K^T
         const uint32_t idesc = kIdescBase<BF16> | (a.scale < 0.f ? 1u << 13 : 0u) | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);  // bit 13: A negated
         const uint32_t q_desc = desc_lower(smem + L::kQ, 16), k_desc = desc_lower(smem + L::kRing, 16);
-        uint32_t it = 0, n_s = 0, n_unit = 0;
-        bool ok = true, fresh = true;
+        uint32_t n_s = 0, n_unit = 0;
+        Ring<kStages> at;  // keys of step j are item 2 j - 1, the first ones item 0
+        bool ok = true, fresh = true, begun = false;
         while (ok && next_step()) {
             const int flags = __shfl_sync(0xffffffffu, steps[n_step % kSteps].flags, 0);
             done_step();
@@ -495,13 +506,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             }
             if (fresh && !(ok = wait_warp(&bar.q_full, n_unit, 55))) break;
             fresh = false;
-            const uint32_t at = it > 0 ? it - 1 : 0, st = at % kStages;
-            if (!(ok = wait_warp(bar.kv_full + st, at / kStages, 54))) break;
+            const uint32_t st = at.stage;
+            if (!(ok = wait_warp(bar.kv_full + st, at.parity, 54))) break;
             const uint32_t k = k_desc + st * (L::kTileBytes >> 4);
 #pragma unroll 1  // the instructions of the roles that run together have to fit into the caches for them
             for (int s = 0; s < 2; ++s) {
                 if (!(flags & (kSlot0 << s))) continue;
-                if (n_s > 0 && !(ok = wait_warp(&bar.s_free, n_s - 1, 56))) break;
+                if (!(ok = wait_warp(&bar.s_free, n_s - 1, 56))) break;
                 ++n_s;
                 tcgen05_fence_after();
                 const uint32_t q = q_desc + (flags & kByKeys ? 0 : s) * (L::kTileBytes >> 4);
@@ -516,13 +527,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 commit_elected(bar.s_full + s);
             }
             if (ok) commit_elected(bar.kv_empty + st);
-            it += 2;
+            at.forward(begun ? 2 : 1), begun = true;
         }
         } else if (warp == 10) {
         // ------------------------------------------------------------ O += P V, in binary16
         constexpr uint32_t kIdesc = kIdescBase<false> | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
         const uint32_t v_desc = desc_lower(smem + L::kRing, kPieceBytes);
-        uint32_t it = 2, n_unit = 0, phase_p = 0, fresh = 3;  // bit s: slot s
+        uint32_t n_unit = 0, phase_p = 0, fresh = 3;  // bit s: slot s
+        Ring<kStages> at;  // values of step j are item 2 j + 2
+        at.forward(2);
         bool ok = true;
         while (ok && next_step()) {
             const int flags = __shfl_sync(0xffffffffu, steps[n_step % kSteps].flags, 0);
@@ -533,14 +546,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 fresh = 3, ++n_unit;
                 continue;
             }
-            const uint32_t st = it % kStages;
-            if (!(ok = wait_warp(bar.kv_full + st, it / kStages, 57))) break;
+            const uint32_t st = at.stage;
+            if (!(ok = wait_warp(bar.kv_full + st, at.parity, 57))) break;
             const uint32_t v = v_desc + st * (L::kTileBytes >> 4);
 #pragma unroll 1
             for (int s = 0; s < 2; ++s) {
                 if (!(flags & (kSlot0 << s))) continue;
                 const uint32_t first = (fresh >> s) & 1u;
-                if (first && n_unit > 0 && !(ok = wait_warp(bar.o_empty + s, n_unit - 1, 58))) break;
+                if (first && !(ok = wait_warp(bar.o_empty + s, n_unit - 1, 58))) break;
                 fresh &= ~(1u << s);
 #pragma unroll 1
                 for (int half = 0; half < 2 && ok; ++half) {
@@ -557,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 commit_elected(bar.o_done + s);
             }
             if (ok) commit_elected(bar.kv_empty + st);
-            it += 2;
+            at.forward(2);
         }
         }
     } else if (warp >= 12) {
@@ -569,19 +582,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         constexpr int kPer = D / 8, kRows = 128 / kPer;  // threads of a token, tokens side by side
         const int row0 = t / kPer, c = t % kPer;
         const uint32_t to0 = smem_u32(smem + L::kRing + (c / 8) * kPieceBytes + row0 * 128 + (((c & 7) ^ (row0 & 7)) << 4));
-        uint32_t n_raw = 0, n_k = 0;  // items so far, keys among them
-        bool ok = true;
+        uint32_t n_raw = 0;
+        Ring<kStages> at;
+        bool ok = true, begun = false;
         while (ok && next_step()) {
             const int flags = steps[n_step % kSteps].flags;
             done_step();
             if (flags & kEnd) continue;
-            if ((flags & kExit) && n_k == 0) break;
+            if ((flags & kExit) && !begun) break;
 #pragma unroll 1
-            for (int kv = flags & kExit ? 1 : 0; kv < (n_k == 0 ? 1 : 2); ++kv, ++n_raw) {
-                const uint32_t at = kv == 0 ? max(2 * n_k, 1u) - 1 : 2 * n_k;  // n_k: with kv = 1 the step is not counted yet
-                const uint32_t rs = n_raw % kRaw, st = at % kStages;
+            for (int kv = flags & kExit ? 1 : 0; kv < (begun ? 2 : 1); ++kv, ++n_raw) {
+                if (flags & kExit) at.forward(1);  // the last values' item is behind that of keys that there are none of
+                const uint32_t rs = n_raw % kRaw, st = at.stage;
                 if (!(ok = wait_warp(bar.raw_full + rs, n_raw / kRaw, 59))) break;
-                if (at >= kStages && !(ok = wait_warp(bar.kv_empty + st, at / kStages - 1, 65))) break;
+                if (!(ok = wait_warp(bar.kv_empty + st, at.parity ^ 1u, 65))) break;
                 uint32_t from = smem_u32(smem + L::kRawRing + rs * L::kRawBytes + t * 8);
                 uint32_t to = to0 + st * L::kTileBytes;  // a thread's rows are a multiple of 8 apart: the swizzle is the same for all
                 // Short loops, whose instructions stay next to the scheduler: unrolled eight times this took three times as long, most of it
@@ -620,8 +634,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar.raw_empty + rs), mbar_arrive(bar.kv_full + st);
+                at.forward(1);
             }
-            ++n_k;
+            begun = true;
             if (flags & kExit) break;
         }
     } else {
@@ -656,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 if (tainted) sum = __int_as_float(0x7fc00000);
                 if (by_keys && s == 1) {
                     // slot 0 has read what is there from the unit before
-                    if (n_unit > 0 && !(ok = wait_warp(bar.o_empty + 1, n_unit - 1, 66))) break;
+                    if (!(ok = wait_warp(bar.o_empty + 1, n_unit - 1, 66))) break;
                     sums[row] = make_float2(taken ? m : -INFINITY, taken ? sum : 0.f);
                     if (row == 0) *sums_ref = ref;
                     __syncwarp();
@@ -739,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             tcgen05_fence_after();
             const int shift = by_keys ? 0 : s * slot_tokens;
             // Before O is rescaled or P written the product with the tile before has to be done.
-            bool may_write = n_s == 0;
+            bool may_write = false;
             auto until_done = [&]() {
                 if (!may_write) {
                     may_write = wait_warp(bar.o_done + s, n_s - 1, 61);
