@@ -489,7 +489,7 @@ pd_status pd_rope_bf16(const void *q, int64_t q_token_stride, int64_t q_head_str
                        void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
- * pd_kv_append_rope -- turns queries and keys and quantises the turned keys and the values into the cache, in one launch.
+ * pd_kv_append_rope -- turns queries and keys and quantises the turned keys and the values into the cache.
  *
  *   q, q_out : queries, turned into q_out (which may be q itself) in the rows that a sequence claims; not looked at where q_heads is 0
  *   positions : NULL: a token turns with its place in its sequence, seq_lens[b] - (cu_seqlens[b + 1] - cu_seqlens[b]) for the first new one

@@ -1,4 +1,4 @@
-// Rotating queries and keys and writing keys and values into the 8-bit paged cache, in one launch.
+// Rotating queries and keys and writing keys and values into the 8-bit paged cache.
 //
 // Rotation as in pd_rotate.cuh, codes and scales as in pd_kv_append; a rotated key is quantised from binary32, without a rounding to 16
 // bits between.  Bound by memory: a query 2 bytes in and out, a key or value 2 bytes in and 1 out (3 with the values handed back).
@@ -6,17 +6,20 @@
 // Three kinds of blocks in one grid:
 //   few    : sequences with at most kFew new tokens, a warp for the keys or values of a head with all of its tokens in registers; the
 //            block computes the angles of the tokens together
-//   pages  : longer pieces, a page (kSub threads, two items of 16 values a thread) walks over several heads, so that the angles, which
+//   pages  : longer pieces, a page (two items of 16 values a thread) walks over several heads, so that the angles, which
 //            stay in registers, are computed once for all of them; the next head's values are on their way while this one's largest
 //            magnitude is found
-//   queries: a token of all query heads each
+//   queries: a token of all query heads each, where they are few; many of them have a launch of their own
 // A sequence is in the hands of the first or the second kind by its own length, whatever the others of the call are.
+#include <type_traits>
+
 #include "pd_kv_quant.cuh"
 #include "pd_rotate.cuh"
 
 namespace pd {
 namespace {
 
+constexpr int64_t kManyQueries = 1 << 20;  // values
 constexpr int kFew = 8;  // tokens: as many as two items a lane hold at head_dim 128
 
 // 16 values to their codes and, unless nullptr, to the values that those stand for; at0 and at1 as in Item
@@ -62,15 +65,30 @@ __device__ __forceinline__ int last_at_or_before(int n, int id, Key key) {
     return b;
 }
 
+// A token's queries; rows that no sequence claims stay as they are.
+template <int D, bool BF16, bool INTERLEAVED>
+__device__ __forceinline__ void turn_queries(const AppendRopeArgs &args, int token, float2 *cs) {
+    const AppendArgs &a = args.a;
+    const HeadsView x[2] = {args.q, {}}, out[2] = {args.q_out, {}};
+    const int heads[2] = {args.q_heads, 0};
+    turn_token<D, BF16, INTERLEAVED>(x, out, heads, token, args.r, cs, a.status, [&](int &place) {
+        const int b = last_at_or_before(a.n_seqs, token, [&](int i) { return __ldg(a.cu_seqlens + i); });
+        const int first = __ldg(a.cu_seqlens + b), last = __ldg(a.cu_seqlens + b + 1);
+        place = __ldg(a.seq_lens + b) - last + token;
+        return token >= first && token < last;
+    });
+}
+
 struct Grid {
-    int few, pages, head_chunks, chunk_heads;  // blocks of the first two kinds; heads that a page block walks over
+    int few, queries, head_chunks, chunk_heads;  // blocks of the first two kinds; heads that a page block walks over
+    bool by_tokens;                              // how sequences are told from a page block's number
 };
 
-// page 64 with heads of 64 and 128: 128 and 256 threads; a block has as many pages' or heads' worth of them as fit
+// page 64 with heads of 64 and 128: 128 and 256 threads; a block has as many heads' worth of them as fit
 __host__ __device__ constexpr int sub_threads(int D, int page) { return page * D / 32; }
 
-template <int D, bool BF16, bool INTERLEAVED>
-__global__ void __launch_bounds__(512) append_rope_kernel(const AppendRopeArgs args, const Grid grid) {
+template <int D, bool BF16, bool INTERLEAVED, int THREADS, bool QUERIES>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS) append_rope_kernel(const AppendRopeArgs args, const Grid grid) {
     constexpr int kItems = D / 16;  // of a head
     const AppendArgs &a = args.a;
     const Rotation &r = args.r;
@@ -152,18 +170,27 @@ __global__ void __launch_bounds__(512) append_rope_kernel(const AppendRopeArgs a
         return;
     }
     id -= grid.few;
-
-    if (id < grid.pages) {
+    if (QUERIES && id < grid.queries) {
+        turn_queries<D, BF16, INTERLEAVED>(args, id, cs);
+        return;
+    }
+    if (QUERIES) id -= grid.queries;
+    {
         // ------------------------------------------------------------ a page of a longer piece: keys or values of several heads
         const int page = 1 << a.page_log2, sub_size = sub_threads(D, page), subs = blockDim.x / sub_size;
         const int sub = threadIdx.x / sub_size, t = threadIdx.x - sub * sub_size;
         const int chunk = id % grid.head_chunks, which = (id / grid.head_chunks) & 1, slot = id / grid.head_chunks >> 1;
-        // Sequence b's pages are the ids from cu[b] / page + 2 b on: there are never more of them than ids before the next sequence's.
-        const int b = last_at_or_before(a.n_seqs, slot, [&](int i) { return (min(max(__ldg(a.cu_seqlens + i), 0), a.n_tokens) >> a.page_log2) + 2 * i; });
+        // Sequence b's pages are the ids from cu[b] / page + 2 b on, or, where there are more sequences than could have a long piece, from
+        // cu[b] (1 / page + 2 / 9) on: n tokens, 9 at least, touch (n - 1) / page + 2 pages at most, never more than ids before the next sequence's.
+        auto first_id = [&](int i) {
+            const int64_t at = min(max(__ldg(a.cu_seqlens + i), 0), a.n_tokens);
+            return static_cast<int>(grid.by_tokens ? (at * (2 * page + kFew + 1) >> a.page_log2) / (kFew + 1) : (at >> a.page_log2) + 2 * static_cast<int64_t>(i));
+        };
+        const int b = last_at_or_before(a.n_seqs, slot, first_id);
         const int first = __ldg(a.cu_seqlens + b), last = __ldg(a.cu_seqlens + b + 1), len = __ldg(a.seq_lens + b);
         if (bad_lengths(a, first, last, len) || last - first <= kFew) return;  // reported, and taken, by the first kind
         const int pos0 = len - (last - first);
-        const int pi = (pos0 >> a.page_log2) + slot - ((first >> a.page_log2) + 2 * b);
+        const int pi = (pos0 >> a.page_log2) + slot - first_id(b);
         const int64_t page_start = static_cast<int64_t>(pi) << a.page_log2;
         const int lo = static_cast<int>(max(static_cast<int64_t>(pos0), page_start));
         const int hi = static_cast<int>(min(static_cast<int64_t>(len), page_start + page));
@@ -228,19 +255,17 @@ __global__ void __launch_bounds__(512) append_rope_kernel(const AppendRopeArgs a
                                      values ? values + ((tok0 + tok + i * far) * a.kv_heads + head) * D : nullptr, item.at0, item.at1);
             if (t == 0) *scale = sc.s;
         }
-        return;
     }
-    id -= grid.pages;
+}
 
-    // ---------------------------------------------------------------- a token's queries; rows that no sequence claims stay as they are
-    const HeadsView x[2] = {args.q, {}}, out[2] = {args.q_out, {}};
-    const int heads[2] = {args.q_heads, 0};
-    turn_token<D, BF16, INTERLEAVED>(x, out, heads, id, r, cs, a.status, [&](int &place) {
-        const int b = last_at_or_before(a.n_seqs, id, [&](int i) { return __ldg(a.cu_seqlens + i); });
-        const int first = __ldg(a.cu_seqlens + b), last = __ldg(a.cu_seqlens + b + 1);
-        place = __ldg(a.seq_lens + b) - last + id;
-        return id >= first && id < last;
-    });
+// The same for many tokens, in a kernel of its own: with the registers of the one above too few values would be on their way.
+constexpr int kQueryThreads = 256;
+template <int D, bool BF16, bool INTERLEAVED>
+__global__ void __launch_bounds__(kQueryThreads) queries_rope_kernel(const AppendRopeArgs args) {
+    __shared__ float2 cs[D / 2];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    turn_queries<D, BF16, INTERLEAVED>(args, blockIdx.x, cs);
 }
 
 template <int D, bool BF16>
@@ -249,21 +274,26 @@ pd_status launch(const AppendRopeArgs &args, bool interleaved, cudaStream_t stre
     const int page = 1 << a.page_log2, threads = max(256, sub_threads(D, page)), subs = threads / sub_threads(D, page);
     const int warps = threads / 32;
     const int64_t few = static_cast<int64_t>(a.n_seqs) * ((2 * a.kv_heads + warps - 1) / warps);
-    Grid grid = {static_cast<int>(few), 0, 1, a.kv_heads};
+    const bool apart = static_cast<int64_t>(a.n_tokens) * args.q_heads * D >= kManyQueries;
+    Grid grid = {static_cast<int>(few), args.q_heads && !apart ? a.n_tokens : 0, 1, a.kv_heads, false};
+    int64_t page_blocks = 0;
     if (a.n_tokens > kFew) {
-        // Longer walks compute fewer angles, more blocks fill the GPU: as long a walk as leaves four blocks for each SM.
-        const int64_t slots = a.n_tokens / page + 2 * static_cast<int64_t>(a.n_seqs), used = a.n_tokens / page + 1;
+        // Longer walks compute fewer angles, more blocks fill the GPU: as long a walk as leaves four blocks for each SM
+        // (2048 tokens, 32 heads of 128, us with 2, 4, 8, 16: 40, 38, 41, 50;  9009 tokens, 8 heads: 84, 88, 90, 103).
+        grid.by_tokens = 2 * a.n_tokens < (kFew + 1) * 2 * static_cast<int64_t>(a.n_seqs);
+        const int64_t used = a.n_tokens / page + 1;
+        const int64_t slots = grid.by_tokens ? static_cast<int64_t>(a.n_tokens) * (2 * page + kFew + 1) / ((kFew + 1) * page) + 1 : used + 2 * static_cast<int64_t>(a.n_seqs);
         int64_t chunks = (4 * static_cast<int64_t>(sm_count()) + 2 * used - 1) / (2 * used);
         const int64_t most = (a.kv_heads + subs - 1) / subs;
         chunks = chunks < most ? chunks : most;
         grid.chunk_heads = static_cast<int>((most + chunks - 1) / chunks) * subs;
         grid.head_chunks = (a.kv_heads + grid.chunk_heads - 1) / grid.chunk_heads;
         if (slots * 2 * grid.head_chunks + few + a.n_tokens > INT32_MAX / 2) return PD_ERR_UNSUPPORTED_SHAPE;
-        grid.pages = static_cast<int>(slots * 2 * grid.head_chunks);
+        page_blocks = slots * 2 * grid.head_chunks;
     }
     if (few > INT32_MAX / 4) return PD_ERR_UNSUPPORTED_SHAPE;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(grid.few + grid.pages + (args.q_heads ? a.n_tokens : 0)));
+    cfg.gridDim = dim3(static_cast<unsigned>(grid.few + grid.queries + page_blocks));
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -272,8 +302,20 @@ pd_status launch(const AppendRopeArgs &args, bool interleaved, cudaStream_t stre
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     count_launch();
-    return cuda_ok(interleaved ? cudaLaunchKernelEx(&cfg, append_rope_kernel<D, BF16, true>, args, grid)
-                               : cudaLaunchKernelEx(&cfg, append_rope_kernel<D, BF16, false>, args, grid));
+    auto pick = [&](auto queries) {
+        constexpr bool Q = decltype(queries)::value;
+        return threads == 256 ? (interleaved ? append_rope_kernel<D, BF16, true, 256, Q> : append_rope_kernel<D, BF16, false, 256, Q>)
+                              : (interleaved ? append_rope_kernel<D, BF16, true, 512, Q> : append_rope_kernel<D, BF16, false, 512, Q>);
+    };
+    const auto kernel = apart ? pick(std::false_type()) : pick(std::true_type());
+    if (cudaLaunchKernelEx(&cfg, kernel, args, grid) != cudaSuccess)
+        return PD_ERR_CUDA;
+    if (!apart) return PD_OK;
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_tokens));
+    cfg.blockDim = dim3(static_cast<unsigned>(turn_threads(args.q_heads, D, kQueryThreads)));
+    count_launch();
+    return cuda_ok(interleaved ? cudaLaunchKernelEx(&cfg, queries_rope_kernel<D, BF16, true>, args)
+                               : cudaLaunchKernelEx(&cfg, queries_rope_kernel<D, BF16, false>, args));
 }
 
 }  // namespace

@@ -19,10 +19,9 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a) {
 
 template <int D, bool BF16>
 pd_status launch(const RopeArgs &a, bool interleaved, cudaStream_t stream) {
-    const int items = (a.heads[0] + a.heads[1]) * (D / 16);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(a.n_tokens));
-    cfg.blockDim = dim3(static_cast<unsigned>(items < kThreads ? (items + 31) / 32 * 32 : kThreads));
+    cfg.blockDim = dim3(static_cast<unsigned>(turn_threads(a.heads[0] + a.heads[1], D, kThreads)));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -127,4 +127,10 @@ __device__ __forceinline__ void turn_token(const HeadsView (&x)[2], const HeadsV
     for (; h < all; h += step) finish(h, load16(from(x, h), item.at0, item.at1));
 }
 
+// Threads of such a block: rounds over the heads that are all full, if that is possible.
+inline int turn_threads(int heads, int head_dim, int most) {
+    const int items = head_dim / 16, rounds = (heads * items + most - 1) / most;
+    return ((heads + rounds - 1) / rounds * items + 31) / 32 * 32;
+}
+
 }  // namespace pd
