@@ -524,6 +524,8 @@ pd_status pd_kv_append_rope_bf16(const void *q, int64_t q_token_stride, int64_t 
  *   out : out, [n_tokens, q_heads, head_dim]: token i of the n new ones attends to the cached tokens 0 .. seq_lens[b] - n + i
  * Rows of n_tokens that no sequence claims are left as they are.  Slots of a page behind what a token attends to and pages that it does not
  * reach have no influence on it, whatever they hold; a page whose scale is not finite makes the tokens that attend to any of it NaN.
+ * The cache holds fewer than 2^31 blocks of 16 tokens and one head (n_pages * kv_heads * page / 16).  Scores are any finite size; the sums of a query
+ * times codes have to be finite in binary32 (magnitudes below 2^113).
  * Weights are rounded to binary16 (relative to the largest, times the scale of V's page, times 2^7) for their product with V; pages whose scale of V is below 2^-67 of the
  * largest of the sequence lose precision.  Offsets that decrease, more new tokens than max_new or than seq_lens[b] and lengths beyond the table
  * latch PD_ERR_BAD_INDEX, and the sequence is left out.  The same call gives the same bits.

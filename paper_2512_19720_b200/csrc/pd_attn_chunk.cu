@@ -17,6 +17,16 @@
 // The keys of all units, one unit after another, are dealt to the blocks in ranges of equal cost whatever the lengths are; where a
 // range ends inside a unit the parts are joined by a second kernel, in the order of the keys: results do not depend on the schedule.
 //
+// Bound.  By rows a tile of 128 keys is 2048 clocks of products and 2048 of the 16 exponentials a clock that an SM has, by keys the 32 KB of its
+// codes, 1370 clocks of the SM's share of the memory.  Measured: 2048 tokens behind 16384, 64 heads on 8: 1.28 ms, 0.91 PFLOP/s, 4700 clocks a
+// tile; 64 sequences of 4 tokens, 288 thousand keys (600 MB): 265 us, 4000 clocks a tile.  By rows the softmax's warps are busy all the time: half
+// with the exponentials of both slots, half with the latencies of waits, loads and scales between them.  By keys it is the conversion: 16 KB
+// of codes take 900 to 1200 clocks, two of them a tile, with 300 clocks of waits each; its 64 KB of stores alone keep the shared memory busy
+// for 600.  Both suffer when the code of the 16 warps' roles does not fit into the SM's cache for instructions: the waits, loops and rings
+// are written for that (counters: warps that wait for instructions 1.2 -> 0.3 an issue, 1.33 -> 1.27 ms).
+// Tried and dropped: P in the place of the scores with both passes over them from tensor memory in loops (1.46 ms), two threads a row (2.5 ms: 24
+// warps), 8 warps for the conversion (no change), codes through registers instead of a ring in shared memory (1.75 ms, code too long).
+//
 // Roles: warps 0-3 and 4-7 the softmax of slot 0 and 1, and the outputs; warp 8 units and pages; warp 11 copies; warps 9 and 10 the products with the keys
 // and with the values; warps 12-15 turn codes into 16-bit operands.  Every wait on another role is bounded.
 #include "pd_attn.cuh"
@@ -598,8 +608,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 if (!(ok = wait_warp(bar.kv_empty + st, at.parity ^ 1u, 65))) break;
                 uint32_t from = smem_u32(smem + L::kRawRing + rs * L::kRawBytes + t * 8);
                 uint32_t to = to0 + st * L::kTileBytes;  // a thread's rows are a multiple of 8 apart: the swizzle is the same for all
-                // Short loops, whose instructions stay next to the scheduler: unrolled eight times this took three times as long, most of it
-                // waiting for instructions.  Loads are ahead of the stores, which the compiler would not let them pass.
+                // A short loop: eight loads and conversions written out take 500 clocks for 16 KB instead of 735 where nothing else runs, but
+                // here the other roles' instructions then have to be fetched again and again (64 sequences of 4 tokens: 300 us beside 267).
+                // Loads are ahead of the stores, which they must not pass.
                 auto convert = [&](auto codes4) {
                     uint2 x = lds64(from), y = lds64(from + kRows * D);
 #pragma unroll 1

@@ -1,7 +1,10 @@
 // Rotary positions with one or several axes: queries and keys of a token turn by the same angles in every head.
 //
 // Bound by memory: 2 bytes in and 2 bytes out per value.  A block takes a token with all its heads, so that each angle (a product
-// in 64 bits, a sine and a cosine) is computed once a token; the values are on their way meanwhile.
+// in 64 bits, a sine and a cosine) is computed once a token; the values are on their way meanwhile.  As many threads as the heads keep
+// busy in whole rounds.  Measured: 8160 tokens with 72 heads of 128 56 us (5.4 TB/s; 64 us with 256 threads, a quarter of them idle in the last
+// round), 2048 tokens with 64 heads 17.3 us, where the start of a block (positions, then angles, then the first store) counts.  Blocks that
+// go on with another token, its values under way: 95 and 19 us, since fewer values are on their way.
 #include "pd_rotate.cuh"
 
 namespace pd {

@@ -87,6 +87,7 @@ def test_refusals(api, suffix):
     assert call(chunk, CHUNK, q_heads=12) == INVALID
     assert call(chunk, CHUNK, scale=float("inf")) == INVALID
     assert call(chunk, CHUNK, max_new=-1) == INVALID
+    assert call(chunk, CHUNK, n_pages=(1 << 31) // 8) == SHAPE and call(chunk, CHUNK, n_pages=1 << 60) == SHAPE
     # nothing to do: no launch, and empty tensors may have no address
     assert call(rope, ROPE, n_tokens=0, q=None, k=None, q_out=None, k_out=None, positions=None) == 0
     assert call(append, APPEND, n_tokens=0, q=None, k=None, v=None, q_out=None, positions=None) == 0
