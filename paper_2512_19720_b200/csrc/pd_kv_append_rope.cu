@@ -23,7 +23,9 @@
 namespace pd {
 namespace {
 
-constexpr int64_t kManyQueries = 1 << 25;  // values
+// Values of queries from which on they get a launch of their own, where more of them are under way: 9009 tokens with 64 heads of 128 88 us beside
+// 102; 2048 tokens with 32 heads 38 us beside 35, where the second launch's start costs more.
+constexpr int64_t kManyQueries = 1 << 25;
 constexpr int kFew = 8;  // tokens: as many as two items a lane hold at head_dim 128
 
 // 16 values to their codes and, unless nullptr, to the values that those stand for; at0 and at1 as in Item
@@ -86,6 +88,7 @@ __device__ __forceinline__ void turn_queries(const AppendRopeArgs &args, int tok
 struct Grid {
     int few, queries, head_chunks, chunk_heads;  // blocks of the first two kinds; heads that a page block walks over
     bool by_tokens;                              // how sequences are told from a page block's number
+    int pages_first;                             // so many page blocks stand before the queries': all where long pieces are likely, or none
 };
 
 // page 64 with heads of 64 and 128: 128 and 256 threads; a block has as many heads' worth of them as fit
@@ -174,11 +177,14 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) append_rope_kernel(con
         return;
     }
     id -= grid.few;
-    if (QUERIES && id < grid.queries) {
-        turn_queries<D, BF16, INTERLEAVED>(args, id, cs);
-        return;
+    if (QUERIES && id >= grid.pages_first) {
+        id -= grid.pages_first;
+        if (id < grid.queries) {
+            turn_queries<D, BF16, INTERLEAVED>(args, id, cs);
+            return;
+        }
+        id -= grid.queries;
     }
-    if (QUERIES) id -= grid.queries;
     {
         // ------------------------------------------------------------ a page of a longer piece: keys or values of several heads
         const int page = 1 << a.page_log2, sub_size = sub_threads(D, page), subs = blockDim.x / sub_size;
@@ -279,7 +285,7 @@ pd_status launch(const AppendRopeArgs &args, bool interleaved, cudaStream_t stre
     const int warps = threads / 32;
     const int64_t few = static_cast<int64_t>(a.n_seqs) * ((2 * a.kv_heads + warps - 1) / warps);
     const bool apart = static_cast<int64_t>(a.n_tokens) * args.q_heads * D >= kManyQueries;
-    Grid grid = {static_cast<int>(few), args.q_heads && !apart ? a.n_tokens : 0, 1, a.kv_heads, false};
+    Grid grid = {static_cast<int>(few), args.q_heads && !apart ? a.n_tokens : 0, 1, a.kv_heads, false, 0};
     int64_t page_blocks = 0;
     if (a.n_tokens > kFew) {
         // Longer walks compute fewer angles, more blocks fill the GPU: as long a walk as leaves four blocks for each SM
@@ -294,6 +300,7 @@ pd_status launch(const AppendRopeArgs &args, bool interleaved, cudaStream_t stre
         grid.head_chunks = (a.kv_heads + grid.chunk_heads - 1) / grid.chunk_heads;
         if (slots * 2 * grid.head_chunks + few + a.n_tokens > INT32_MAX / 2) return PD_ERR_UNSUPPORTED_SHAPE;
         page_blocks = slots * 2 * grid.head_chunks;
+        grid.pages_first = grid.by_tokens ? 0 : static_cast<int>(page_blocks);
     }
     if (few > INT32_MAX / 4) return PD_ERR_UNSUPPORTED_SHAPE;
     cudaLaunchConfig_t cfg = {};
