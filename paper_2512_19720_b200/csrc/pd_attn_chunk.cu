@@ -687,6 +687,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     if (row == 0) *sums_ref = ref;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bar.joined);
+                    // Slot 0 writes the output.  This one waits too: a barrier tells two phases apart, so that nobody may leave one out.
+                    if (!(ok = wait_warp(&bar.o_last, n_unit, 69))) break;
                 } else {
                     float w0 = taken ? 1.f : 0.f, w1 = 0.f;  // weights of the slots' sums
                     int at = ref;

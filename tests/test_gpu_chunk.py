@@ -135,6 +135,17 @@ def test_chunk_split_over_blocks(api, held, new, hq, hkv, d):
     check(api, pages, queries(sum(new), hq, d, torch.float16, 31), lens, new, 0.05, only=only)
 
 
+def test_chunk_short_units_of_both_kinds_again_and_again(api):
+    """Units of one to four tiles, some whose slots hold the same rows and some whose do not, in turn: the same bits every time."""
+    for hq, hkv, new, held in ((10, 2, [1, 0, 7, 65, 200], 250), (8, 8, [130, 257, 5, 140], 0), (16, 4, [40, 33, 70, 3, 65] * 4, 60)):
+        lens = [n + held for n in new]
+        pages = Pages(lens, hkv, 128, 128, 83)
+        q = queries(sum(new), hq, 128, torch.bfloat16, 5)
+        first = check(api, pages, q, lens, new)
+        for _ in range(100):
+            assert torch.equal(first, api.pd_attn_chunk(q, *pages.tensors(), offsets(new), i32(lens), pages.block_table))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_chunk_many_sequences(api, dtype):
     rng = np.random.default_rng(37)
