@@ -818,6 +818,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 for (int k = 1; k < 15; k += 2) top = max3(top, __uint_as_float(w[k]), __uint_as_float(w[k + 1]));
                 best = fmaxf(best, top * st.factor[g].x);
             }
+            // Rows that stand for nothing, which hold anything, have no say in when the others' maxima move: their bits would depend on it.
+            if (my_token >= min(slot_tokens, st.n_tokens - shift)) best = -INFINITY;
             const int new_ref = st.ref;
             if (__any_sync(0xffffffffu, best - m > kMaxLead) || new_ref != ref) {
                 if (!(ok = until_done())) break;
