@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         for (int i = 0; i < kStages; ++i) mbar_init(bar.kv_full + i, 4), mbar_init(bar.kv_empty + i, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(bar.s_full + s, 1), mbar_init(bar.p_half[s], 4), mbar_init(bar.p_half[s] + 1, 4);
-            mbar_init(bar.o_done + s, 1), mbar_init(bar.o_empty + s, 4);
+            mbar_init(bar.o_done + s, 1), mbar_init(bar.o_empty + s, s == 0 ? 4 : 8);
         }
         mbar_init(&bar.q_full, 1), mbar_init(&bar.q_empty, 1), mbar_init(&bar.s_free, 4), mbar_init(&bar.o_last, 1), mbar_init(&bar.joined, 4);
         bar.abort_flag = 0;
@@ -552,6 +552,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             done_step();
             if (flags & kExit) break;
             if (flags & kEnd) {
+                // The softmax's warps read one phase of o_last a unit and arrive on o_empty behind it: the next one must not end before all have,
+                // those of a slot that no tile of the unit belonged to among them.
+#pragma unroll 1
+                for (int s = 0; s < 2 && ok; ++s)
+                    if ((fresh >> s) & 1u) ok = wait_warp(bar.o_empty + s, n_unit - 1, 67);
+                if (!ok) break;
                 commit_elected(&bar.o_last);
                 fresh = 3, ++n_unit;
                 continue;
@@ -687,8 +693,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     if (row == 0) *sums_ref = ref;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bar.joined);
-                    // Slot 0 writes the output.  This one waits too: a barrier tells two phases apart, so that nobody may leave one out.
+                    // Slot 0 writes the output.  This one waits too, and says that it has: a barrier tells two phases apart, so that nobody may
+                    // leave one out or come late.
                     if (!(ok = wait_warp(&bar.o_last, n_unit, 69))) break;
+                    if (lane == 0) mbar_arrive(bar.o_empty + 1);
                 } else {
                     float w0 = taken ? 1.f : 0.f, w1 = 0.f;  // weights of the slots' sums
                     int at = ref;
@@ -749,9 +757,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     }
                     tcgen05_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
+                    if (lane == 0) {  // slot 1's barrier counts the warps of both slots, or its own ones twice
                         mbar_arrive(bar.o_empty + s);
-                        if (by_keys) mbar_arrive(bar.o_empty + 1);
+                        if (by_keys || s == 1) mbar_arrive(bar.o_empty + 1);
                     }
                 }
                 if (by_keys) ++n_joined;
