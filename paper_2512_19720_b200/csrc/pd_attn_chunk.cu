@@ -552,12 +552,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             done_step();
             if (flags & kExit) break;
             if (flags & kEnd) {
-                // The softmax's warps read one phase of o_last a unit and arrive on o_empty behind it: the next one must not end before all have,
-                // those of a slot that no tile of the unit belonged to among them.
-#pragma unroll 1
-                for (int s = 0; s < 2 && ok; ++s)
-                    if ((fresh >> s) & 1u) ok = wait_warp(bar.o_empty + s, n_unit - 1, 67);
-                if (!ok) break;
                 commit_elected(&bar.o_last);
                 fresh = 3, ++n_unit;
                 continue;
@@ -565,11 +559,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             const uint32_t st = at.stage;
             if (!(ok = wait_warp(bar.kv_full + st, at.parity, 57))) break;
             const uint32_t v = v_desc + st * (L::kTileBytes >> 4);
+            // The softmax's warps read one phase of o_last a unit and arrive on o_empty behind it: the next one must not end before all have,
+            // those of a slot that no tile of the unit belongs to among them.
+            if (fresh == 3) {
+#pragma unroll 1
+                for (int s = 0; s < 2 && ok; ++s) ok = wait_warp(bar.o_empty + s, n_unit - 1, 58);
+                if (!ok) break;
+            }
 #pragma unroll 1
             for (int s = 0; s < 2; ++s) {
                 if (!(flags & (kSlot0 << s))) continue;
                 const uint32_t first = (fresh >> s) & 1u;
-                if (first && !(ok = wait_warp(bar.o_empty + s, n_unit - 1, 58))) break;
                 fresh &= ~(1u << s);
 #pragma unroll 1
                 for (int half = 0; half < 2 && ok; ++half) {
