@@ -63,7 +63,7 @@ struct Step {
     int limit;             // last key that the unit's first token attends to
     int ref;               // r = 2^ref
     int token, n_tokens;   // the unit's first token (row of q) and tokens
-    int head, n_heads;     // first query head and heads of the rows
+    int head, done_heads;  // first query head of the rows, and heads from it on that are another unit's
     int part;              // where a part of a unit goes; -1: the whole unit, written to out
     int tainted;           // first key of a page whose scale is not finite
     int pad[2];
@@ -299,8 +299,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 const int t0 = at.tile, t1 = last_unit ? end.tile : tiles;
                 if (t0 < t1) {
                     const bool by_keys = s.by_keys(at.unit);
-                    const int kvh = at.stream / chunks, head = kvh * group + (at.stream - kvh * chunks) * heads;
-                    const int n_heads = min(heads, (kvh + 1) * group - head);
+                    // Shares that do not divide the group evenly overlap: every row has a query of this key/value head, or none of the unit's tokens.
+                    const int kvh = at.stream / chunks, done_heads = max((at.stream - kvh * chunks + 1) * heads - group, 0);
+                    const int head = kvh * group + (at.stream - kvh * chunks) * heads - done_heads;
                     const int token = first + at.unit * s.span, n_tok = min(s.span, s.n - at.unit * s.span);
                     const int limit = static_cast<int>(s.held) + at.unit * s.span;
                     const int last0 = by_keys ? keys - 1 : limit + slot_tokens - 1;  // last key of slot 0's last token
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                         const int slot = t0 > 0 ? 0 : 1;
                         part = blockIdx.x * 2 + slot;
                         header[slot] = t1 == tiles ? 2 : 1;
-                        if (slot == 1) header_unit = make_int4(token, n_tok, head, n_heads);
+                        if (slot == 1) header_unit = make_int4(token, n_tok, head, done_heads);
                     }
                     // A lane knows 16 keys of four tiles, and the page of 16 keys of the next four.
                     const int key_end = min(keys, t1 * kTile);
@@ -404,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                             }
                             if (lane == 0) {
                                 *reinterpret_cast<int4 *>(&st.flags) = make_int4(flags, key0, limit, ref == INT32_MIN ? 0 : ref);
-                                *reinterpret_cast<int4 *>(&st.token) = make_int4(token, n_tok, head, n_heads);
+                                *reinterpret_cast<int4 *>(&st.token) = make_int4(token, n_tok, head, done_heads);
                             }
                             __syncwarp();
                             if (lane == 0) mbar_arrive(bar.step_full + ss);
@@ -417,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     if (!(ok = wait_warp(bar.step_empty + ss, sr - 1, 51))) break;
                     if (lane == 0) {
                         Step &st = steps[ss];
-                        st.flags = kEnd | (by_keys ? kByKeys : 0), st.limit = limit, st.token = token, st.n_tokens = n_tok, st.head = head, st.n_heads = n_heads;
+                        st.flags = kEnd | (by_keys ? kByKeys : 0), st.limit = limit, st.token = token, st.n_tokens = n_tok, st.head = head, st.done_heads = done_heads;
                         st.part = part, st.tainted = tainted;
                         mbar_arrive(bar.step_full + ss);
                     }
@@ -681,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             if (flags & kEnd) {
                 const int token = st.token + (by_keys ? 0 : s * slot_tokens) + my_token, left = st.n_tokens - (by_keys ? 0 : s * slot_tokens);
                 const int head = st.head + my_head, part = st.part;
-                const bool valid = my_token < slot_tokens && my_token < left && my_head < st.n_heads;
+                const bool valid = my_token < slot_tokens && my_token < left && my_head >= st.done_heads;
                 const bool tainted = st.limit + (by_keys ? 0 : s * slot_tokens) + my_token >= st.tainted;
                 done_step();
                 float sum = l.x + l.y;
@@ -928,7 +929,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_chunk_join_kernel(const 
     const bool by_keys = unit.y <= slot_tokens;
     const int row = blockIdx.y * 32 + lane, s = row / kTile, r = row - s * kTile;
     const int my_token = r / heads, my_head = r - my_token * heads, t = s * slot_tokens + my_token;
-    const bool valid = (s == 0 || !by_keys) && my_token < slot_tokens && t < unit.y && my_head < unit.w;
+    const bool valid = (s == 0 || !by_keys) && my_token < slot_tokens && t < unit.y && my_head >= unit.w;
     if (!__syncthreads_or(valid)) return;
     if (warp == 0) {  // parts: block c0's second, then the first ones of the blocks behind it up to the one that ended the unit
         int n = 1;

@@ -31,3 +31,22 @@ def test_units_of_one_tile_behind_each_other(api, between, hq, hkv, d):
     for _ in range(30):
         assert torch.equal(first, api.pd_attn_chunk(q, *pages.tensors(), offsets(new), i32(lens), pages.block_table))
     assert api.pd_device_status(api.chunk_workspace()) == 0
+
+
+@pytest.mark.parametrize("hq,hkv", [(129, 1), (258, 2), (257, 1), (514, 2)])
+@pytest.mark.parametrize("new,held", [([3], [200]), ([5, 1], [60, 1000])], ids=str)
+def test_groups_that_do_not_divide_evenly(api, new, held, hq, hkv):
+    """More than 128 query heads share a key/value head and their last share is smaller: rows that stand for no head hold the next
+    key/value head's queries, or nothing, and have no say."""
+    lens = [a + b for a, b in zip(held, new)]
+    for dtype in TYPES:
+        pages = Pages(lens, hkv, 64, 16, 13)
+        q = queries(sum(new), hq, 64, dtype, 17)
+        first = check(api, pages, q, lens, new)
+        if hkv == 1:
+            continue
+        for other in (float("inf"), -300.0, 300.0):
+            changed = q.clone()
+            changed[:, hq // 2:] *= other
+            got = api.pd_attn_chunk(changed, *pages.tensors(), offsets(new), i32(lens), pages.block_table)
+            assert torch.equal(got[:, :hq // 2], first[:, :hq // 2])
