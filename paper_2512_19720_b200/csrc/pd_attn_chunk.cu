@@ -47,6 +47,7 @@ constexpr float kFar = 1024.f;   // reference maxima from which on scores are ro
 constexpr float kRoom = 7.f;     // P is 2^7 times the weight, and at most 2^15
 constexpr float kSmallestScale = 0x1p-120f;  // a page whose scale is below it counts as zeros
 constexpr int kSpread = 7;       // pages of V whose scale is below 2^-7 of the reference are taken in another step
+constexpr float kLeastShare = 0x1p-60f;  // of the reference: 2^(8 + 7) times it is below half of binary16's smallest number
 constexpr int kMostFall = 60;    // how far the reference may fall: O, in its units, grows by as much
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;  // tensor-memory columns; slot 1: P + 64, O + 128
 
@@ -347,7 +348,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     };
                     auto inverse_ref = [&]() { return ref == INT32_MIN ? 1.f : (ref == 127 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(127 - ref) << 23)); };
                     uint32_t place = kNoKeys;
+                    // Below kLeastShare P is zero in binary16 whatever it is; its reciprocal, which the weights' sum takes it times, stays finite.
                     auto of_group = [&](float k, float v, float rel) {
+                        rel = fmaxf(rel, kLeastShare);
                         return make_float4(fmaxf(f0 * k, 0x1p-149f), v == 0.f ? 0.f : __log2f(rel), v == 0.f ? 1.f : __frcp_rn(rel), __uint_as_float(place));
                     };
                     --quad;

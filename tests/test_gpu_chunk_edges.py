@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_chunk import check, queries
+from test_gpu_chunk import check, definition, f64, queries
 from test_gpu_rope import Pages, i32, offsets
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +50,51 @@ def test_groups_that_do_not_divide_evenly(api, new, held, hq, hkv):
             changed[:, hq // 2:] *= other
             got = api.pd_attn_chunk(changed, *pages.tensors(), offsets(new), i32(lens), pages.block_table)
             assert torch.equal(got[:, :hq // 2], first[:, :hq // 2])
+
+
+# ------------------------------------------------------------------ scales of V at the ends of their range
+def check_what_is_attended_to(api, pages, q, lens, new, max_new=0, scale=None, rows=None):
+    """test_gpu_chunk's bound with nothing in it of keys that a token does not attend to: each of the tokens `rows` as the last one of a sequence."""
+    scale = q.shape[2] ** -0.5 if scale is None else scale
+    got = api.pd_attn_chunk(q, *pages.tensors(), offsets(new), i32(lens), pages.block_table, max_new, scale)
+    assert api.pd_device_status(api.chunk_workspace()) == 0
+    at = 0
+    for b, (n, m) in enumerate(zip(lens, new)):
+        one = Pages.__new__(Pages)
+        one.page, one.codes, one.scales, one.table = pages.page, pages.codes, pages.scales, pages.table[b:b + 1]
+        for i in range(m) if rows is None else [i for i in rows if i < m]:
+            want, bound = definition(one, f64(q[at + i:at + i + 1]), [n - m + i + 1], [1], scale, q.dtype)
+            y = f64(got[at + i:at + i + 1])
+            # what lies beyond 65520 rounds to an infinity in binary16, what may lie on either side of it may be either
+            over = np.abs(want) - 65520 if q.dtype == torch.float16 else np.full_like(want, -1e300)
+            assert np.array_equal(y[over > bound], np.sign(want[over > bound]) * np.inf), (b, i)
+            near = over < -bound
+            off = np.abs(y[near] - want[near]) / bound[near]
+            assert np.all(np.isfinite(y[near])) and np.all(off <= 1.0), (b, i, float(off.max()))
+        at += m
+    return got
+
+
+def with_scales(lens, hkv, d, page, of_pages, seed):
+    """Pages whose values have the scales of_pages[sequence][page of it]; those that do not count are NaN."""
+    pages = Pages(lens, hkv, d, page, seed)
+    pages.scales[1][:] = float("nan")
+    for b, scales in enumerate(of_pages):
+        for i in range(-(-lens[b] // page)):
+            pages.scales[1][int(pages.table[b, i])] = float(np.float32(scales[i]))
+    return pages
+
+
+@pytest.mark.parametrize("hq,hkv,d,new,most", [(4, 2, 128, 3, 0), (40, 2, 64, 3, 0), (4, 2, 128, 3, 3), (4, 4, 64, 3, 16)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_values_with_scales_at_the_ends_of_the_range(api, page, hq, hkv, d, new, most):
+    """Pages of V that are below 2^-120 (zeros), just above it, or up to 2^240 above or below the others, in every order."""
+    n = 12 * page + 3
+    scales = [[2.0 ** -126] * 13, [1e-38, 1.0] + [1e-38] * 11, [1.0] * 6 + [2.0 ** -119] * 7, [2.0 ** -119] * 6 + [1.0] * 7, [3e4] * 8 + [1e-36] * 5,
+              [2.0 ** (16 * (6 - i)) for i in range(13)], [2.0 ** (16 * (i - 6)) for i in range(13)], [1.0, 0.0, 2.0 ** -100, 0.0] * 3 + [1.0],
+              [2.0 ** 100] * 3 + [2.0 ** -100] * 10, [2.0 ** 100] + [2.0 ** -119] * 12, [2.0 ** 119, 2.0 ** -119] * 6 + [1.0], [2.0 ** 60] * 5 + [2.0 ** -20, 2.0 ** 60] * 4]
+    lens = [n] * len(scales)
+    pages = with_scales(lens, hkv, d, page, scales, 5)
+    q = queries(new * len(lens), hq, d, torch.bfloat16, hq)
+    got = check_what_is_attended_to(api, pages, q, lens, [new] * len(lens), most, rows=sorted({0, new // 2, new - 1}))
+    assert bool(torch.isfinite(got.float()).all()) and not got[:new].any()
