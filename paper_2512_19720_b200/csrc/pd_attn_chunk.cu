@@ -6,7 +6,9 @@
 // type, O = P C_v in binary16.  The scales go into the exponents.  With s_k, s_v the scales of a key's page and r a power of two,
 //     P = 2^(f s_k S - m + log2(s_v / r) + 7),   l = sum P r / s_v,   out = r O / l.
 // r is a reference for the pages' scales of V: s_v / r is in [2^-7, 1], so that P stays normal in binary16 where the weight is above 2^-14.
-// Where a tile's pages differ by more than that it is gone through again for the others, which happens to hardly any cache.
+// Where a tile's pages differ by more than that it is gone through again for the others, the smallest first, which happens to hardly any cache.
+// Each row has an r of its own, which follows only where the row attends to a page that is taken: pages of later tokens, however large or
+// small, do nothing to its O.  What a row attends to of its last tile is taken before or with larger pages of that tile.
 //
 // A *unit* is 256 or fewer rows of a sequence and key/value head; a row is a token and one of the query heads that share the head,
 // heads first.  Two slots of 128 rows (the rows that one product of the tensor cores takes) read the same keys:
@@ -47,7 +49,10 @@ constexpr float kFar = 1024.f;   // reference maxima from which on scores are ro
 constexpr float kRoom = 7.f;     // P is 2^7 times the weight, and at most 2^15
 constexpr float kSmallestScale = 0x1p-120f;  // a page whose scale is below it counts as zeros
 constexpr int kSpread = 7;       // pages of V whose scale is below 2^-7 of the reference are taken in another step
-constexpr float kLeastShare = 0x1p-60f;  // of the reference: 2^(8 + 7) times it is below half of binary16's smallest number
+// Shares of the reference that are smaller count as so much: P, 2^(8 + 7) times it at most, is zero in binary16 either way, and the reciprocal, which
+// the weights' sum takes it times, stays finite.
+constexpr float kLeastShare = 0x1p-60f;
+constexpr int kNoRef = -1000;    // of a row that has seen no values but zeros
 constexpr int kMostFall = 60;    // how far the reference may fall: O, in its units, grows by as much
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;  // tensor-memory columns; slot 1: P + 64, O + 128
 
@@ -62,12 +67,13 @@ enum : int { kSlot0 = 1, kSlot1 = 2, kEnd = 4, kExit = 8, kByKeys = 16 };
 struct Step {
     int flags, key0;       // first key of the tile
     int limit;             // last key that the unit's first token attends to
-    int ref;               // r = 2^ref
+    int ref;               // r = 2^ref for the rows that attend to a key from `first_taken` on
     int token, n_tokens;   // the unit's first token (row of q) and tokens
     int head, done_heads;  // first query head of the rows, and heads from it on that are another unit's
     int part;              // where a part of a unit goes; -1: the whole unit, written to out
     int tainted;           // first key of a page whose scale is not finite
-    int pad[2];
+    int first_taken;       // first key, counted from the tile's, whose page's values are not zeros and are taken in this step
+    int pad;
     // for keys 16 g .. 16 g + 15 of the tile
     float4 factor[8];      // of the scores, twice, and log2(s_v / r), twice: pairs as the packed arithmetic takes them
     float weight[8];       // r / s_v
@@ -93,8 +99,8 @@ struct ChunkSmem {
     static constexpr int kRing = 2 * kTileBytes;
     static constexpr int kRawRing = kRing + kStages * kTileBytes;
     static constexpr int kStepRing = kRawRing + kRaw * kRawBytes;
-    static constexpr int kSums = kStepRing + kSteps * static_cast<int>(sizeof(Step));  // m and l of slot 1's rows, by keys
-    static constexpr int kBars = kSums + kTile * 8 + 16;
+    static constexpr int kSums = kStepRing + kSteps * static_cast<int>(sizeof(Step));  // m, l and reference of slot 1's rows, by keys
+    static constexpr int kBars = kSums + kTile * 12;
     static constexpr int kTotal = kBars + 512;
     static constexpr int kScan = kRawRing;  // costs before each thread's share of the sequences, until the first unit is found
     static_assert(sizeof(Bars) <= 512 && kTotal <= 227 * 1024 && (kThreads + kWarps) * 8 <= kRaw * kRawBytes, "shared memory");
@@ -324,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                     int64_t pid = 0;
                     float sk = 0.f, sv = 0.f, sk_next = 0.f, sv_next = 0.f;
                     int pid_next = page_of(quad);
-                    bool good = false;
+                    bool good = false, look = false;
                     auto scales_of = [&](int q, int64_t p, float &k, float &v) {
                         const bool there = q * (4 * kTile) + lane * 16 < key_end;
                         k = v = 0.f;
@@ -332,27 +338,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                         else if (there) k = a.pages[0].scale[p * a.kv_heads + kvh], v = a.pages[1].scale[p * a.kv_heads + kvh];
                     };
                     scales_of(quad, pid_next, sk_next, sv_next);
-                    int tainted = INT32_MAX, ref = INT32_MIN, top = INT32_MIN, turn = 0;
+                    int tainted = INT32_MAX, ref = kNoRef, top = kNoRef, said = kNoRef, turn = 0;  // said: the reference of what was last taken
                     const float f0 = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 0.f;
-                    float4 mine = make_float4(0.f, 0.f, 0.f, 0.f);  // of the lane's 16 keys: factor, log2(s_v / r), r / s_v, place
-                    bool even = false;                              // the scales of the four tiles are near enough for one reference
-                    // the reference for scales of V of which `most` is the largest; true: whatever is below it, down to nothing, is taken with it
-                    auto move_ref = [&](float most, bool fall) {
-                        if (most == 0.f) return true;
-                        const int e = min(static_cast<int>(__float_as_uint(most) >> 23) - 126, 127);  // most <= 2^e
-                        bool all = false;
-                        if (ref == INT32_MIN || e > ref) ref = e;
-                        else if (fall || e <= ref - kSpread) ref = max(e, top - kMostFall), all = ref > e;
-                        top = max(top, ref);
-                        return all;
-                    };
-                    auto inverse_ref = [&]() { return ref == INT32_MIN ? 1.f : (ref == 127 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(127 - ref) << 23)); };
+                    float inverse = 0.f;  // 2^-ref
+                    float4 entry = make_float4(0.f, 0.f, 0.f, 0.f);  // of the lane's 16 keys: factor, log2(s_v / r), r / s_v, place
+                    bool even = false;                               // the four tiles have one reference
+                    unsigned counts = 0;                             // lanes whose keys' values are not zeros and are taken
                     uint32_t place = kNoKeys;
-                    // Below kLeastShare P is zero in binary16 whatever it is; its reciprocal, which the weights' sum takes it times, stays finite.
-                    auto of_group = [&](float k, float v, float rel) {
-                        rel = fmaxf(rel, kLeastShare);
-                        return make_float4(fmaxf(f0 * k, 0x1p-149f), v == 0.f ? 0.f : __log2f(rel), v == 0.f ? 1.f : __frcp_rn(rel), __uint_as_float(place));
-                    };
                     --quad;
                     for (int j = t0; j < t1 && ok; ++j) {
                         if ((j >> 2) != quad) {
@@ -368,35 +360,42 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                             if (!(sv >= kSmallestScale)) sv = 0.f;
                             place = good ? static_cast<uint32_t>((pid * a.kv_heads + kvh) << (a.page_log2 - 4)) + ((lane * 16 & (page - 1)) >> 4) : kNoKeys;
                             if (good && sv == 0.f) place |= kZeroValues;
-                            // positive numbers order like their bits
-                            const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv)));
-                            const float least_v = __uint_as_float(__reduce_min_sync(0xffffffffu, sv == 0.f ? 0x7f800000u : __float_as_uint(sv)));
-                            even = most <= least_v * (1 << (kSpread - 1)) || most == 0.f;
-                            if (even) {
-                                // the reference stays where all scales of the quad are in its range
-                                const float now = inverse_ref();
-                                const bool fall = least_v * now < 1.f / (1 << kSpread);
-                                if (ref == INT32_MIN || most * now > 1.f || fall) even = !move_ref(most, fall) || most == 0.f;
-                                mine = of_group(sk, sv, sv * inverse_ref());
-                            }
+                            even = false, look = true;
                             pid_next = page_of(quad + 1);
                         }
                         const int key0 = j * kTile;
-                        unsigned todo = 0xffu;  // groups of keys that are still to be taken
+                        unsigned todo = 0xffu << (8 * (j & 3));  // lanes whose keys are still to be taken
                         while (todo && ok) {
-                            float4 entry = mine;
-                            const bool holds = (lane >> 3) == (j & 3);  // the lane knows a group of the tile
-                            if (even) {
-                                todo = 0;
+                            if (!even) {
+                                // One reference for all four tiles, or for what one tile has left.  The smallest scales first: what a row attends to of a tile
+                                // is done before or with the larger pages behind it, so that those move no reference that it still needs.
+                                bool now = look || (todo >> lane) & 1u;
+                                // positive numbers order like their bits
+                                const float least = __uint_as_float(__reduce_min_sync(0xffffffffu, now && sv > 0.f ? __float_as_uint(sv) : 0x7f800000u));
+                                const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, now && sv <= least * (1 << (kSpread - 1)) ? __float_as_uint(sv) : 0u));
+                                bool all = false;  // whatever is below the reference, down to nothing, is taken with it
+                                if (most > 0.f && (most * inverse > 1.f || least * inverse < 1.f / (1 << kSpread))) {
+                                    const int e = static_cast<int>(__float_as_uint(most) >> 23) - 126;  // most <= 2^e <= 2^128
+                                    ref = max(e, top - kMostFall), top = max(top, ref), all = ref > e;
+                                    inverse = __uint_as_float(ref < 127 ? static_cast<uint32_t>(127 - ref) << 23 : 1u << (149 - ref));
+                                }
+                                const float rel = sv * inverse, held = fmaxf(rel, kLeastShare);
+                                now = now && (sv == 0.f || (rel <= 1.f && (all || rel >= 1.f / (1 << kSpread))));
+                                const unsigned taken = __ballot_sync(0xffffffffu, now);
+                                counts = __ballot_sync(0xffffffffu, now && sv > 0.f);
+                                if (look) {
+                                    look = false, even = taken == 0xffffffffu;
+                                    if (!even) continue;
+                                }
+                                entry = make_float4(fmaxf(f0 * sk, 0x1p-149f), !now ? -INFINITY : (sv == 0.f ? 0.f : __log2f(held)),
+                                                    !now ? 0.f : (sv == 0.f ? 1.f : __frcp_rn(held)), __uint_as_float(place));
+                                todo &= ~taken;
                             } else {
-                                const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, holds && (todo >> (lane & 7)) & 1u ? __float_as_uint(sv) : 0u));
-                                const bool all = move_ref(most, false);
-                                const float rel = sv * inverse_ref();
-                                const bool now = holds && (todo >> (lane & 7)) & 1u && (all || sv == 0.f || rel >= 1.f / (1 << kSpread));
-                                entry = of_group(sk, sv, rel);
-                                if (!now) entry.y = -INFINITY, entry.z = 0.f;
-                                todo &= ~((__ballot_sync(0xffffffffu, now) >> (8 * (j & 3))) & 0xffu);
+                                todo = 0;
                             }
+                            const bool holds = (lane >> 3) == (j & 3);  // the lane knows a group of the tile
+                            const unsigned mine = (counts >> (8 * (j & 3))) & 0xffu;
+                            if (mine) said = ref;
                             int flags = by_keys ? kByKeys | (turn & 1 ? kSlot1 : kSlot0) : kSlot1 | (key0 <= last0 ? kSlot0 : 0);
                             ++turn;
                             const uint32_t ss = n_step % kSteps, sr = n_step / kSteps;
@@ -407,8 +406,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                                 st.weight[lane & 7] = entry.z, st.place[lane & 7] = __float_as_uint(entry.w);
                             }
                             if (lane == 0) {
-                                *reinterpret_cast<int4 *>(&st.flags) = make_int4(flags, key0, limit, ref == INT32_MIN ? 0 : ref);
+                                *reinterpret_cast<int4 *>(&st.flags) = make_int4(flags, key0, limit, said);
                                 *reinterpret_cast<int4 *>(&st.token) = make_int4(token, n_tok, head, done_heads);
+                                st.first_taken = 16 * (__ffs(mine | 0x100u) - 1);
                             }
                             __syncwarp();
                             if (lane == 0) mbar_arrive(bar.step_full + ss);
@@ -670,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
         float2 *sums = reinterpret_cast<float2 *>(smem + L::kSums);
         int *sums_ref = reinterpret_cast<int *>(smem + L::kSums + kTile * 8);
         uint32_t n_s = 0, n_unit = 0, n_joined = 0;  // steps of the slot, units, units by keys so far
-        int taken = 0, ref = 0;                      // steps of the slot in the unit, its reference
+        int taken = 0, ref = kNoRef;                 // steps of the slot in the unit, the row's reference
         float m = -INFINITY, sub1 = 0.f;
         bool far = false, ok = true;
         float2 l = make_float2(0.f, 0.f);
@@ -693,8 +693,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 if (by_keys && s == 1) {
                     // slot 0 has read what is there from the unit before
                     if (!(ok = wait_warp(bar.o_empty + 1, n_unit - 1, 66))) break;
-                    sums[row] = make_float2(taken ? m : -INFINITY, taken ? sum : 0.f);
-                    if (row == 0) *sums_ref = ref;
+                    sums[row] = make_float2(m, sum);
+                    sums_ref[row] = ref;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bar.joined);
                     // Slot 0 writes the output.  This one waits too, and says that it has: a barrier tells two phases apart, so that nobody may
@@ -710,17 +710,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                         if (other.x != -INFINITY || other.y != 0.f) {  // the same in most rows; a row without anything has nothing to add
                             const float top = fmaxf(m, other.x);
                             const float e0 = m == -INFINITY ? 0.f : exp2_approx(m - top), e1 = other.x == -INFINITY ? 0.f : exp2_approx(other.x - top);
-                            const int other_ref = *sums_ref, most = taken ? max(ref, other_ref) : other_ref;
-                            w0 = taken ? e0 * exp2_approx(static_cast<float>(ref - most)) : 0.f;
-                            w1 = e1 * exp2_approx(static_cast<float>(other_ref - most));
-                            sum = (taken ? sum * e0 : 0.f) + other.y * e1;
-                            m = top, at = most;
+                            const int other_ref = sums_ref[row];
+                            at = max(ref, other_ref);
+                            w0 = e0 * exp2_approx(static_cast<float>(ref - at)), w1 = e1 * exp2_approx(static_cast<float>(other_ref - at));
+                            sum = sum * e0 + other.y * e1;
+                            m = top;
                         }
                     }
                     const bool use0 = __any_sync(0xffffffffu, w0 != 0.f), use1 = __any_sync(0xffffffffu, w1 != 0.f);
                     if (!(ok = wait_warp(&bar.o_last, n_unit, 62))) break;
                     tcgen05_fence_after();
-                    const float scale = __uint_as_float(static_cast<uint32_t>(127 + max(at, -126)) << 23), inv = 1.f / sum;
+                    const float scale = __uint_as_float(static_cast<uint32_t>(126 + max(at, -125)) << 23), inv = 2.f / sum;  // r / 2, which is finite
                     uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(token) * a.out.token_stride + head * a.out.head_stride;
                     float *po = a.partial + static_cast<int64_t>(max(part, 0)) * kPartFloats<D> + ((by_keys ? 0 : s * kTile) + row) * 4;
 #pragma unroll 1
@@ -768,7 +768,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 }
                 if (by_keys) ++n_joined;
                 ++n_unit;
-                taken = 0, m = -INFINITY, l = make_float2(0.f, 0.f);
+                taken = 0, ref = kNoRef, m = -INFINITY, l = make_float2(0.f, 0.f);
                 continue;
             }
             if (!(flags & (kSlot0 << s))) {
@@ -797,6 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                 ++n_s, ++taken;
                 continue;
             }
+            int new_ref = st.ref;
             {
                 const int limit = st.limit + shift + my_token - st.key0;  // last key of the tile that the row attends to
                 const int lowest = __shfl_sync(0xffffffffu, limit, 0);
@@ -812,6 +813,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                         tcgen05_st_32x32b_x32(ts + c, y);
                     }
                     tcgen05_wait_st();
+                    // A reference that moves for pages behind the row's last key is none of its own: O might leave that one's range.
+                    if (limit < st.first_taken || my_token >= min(slot_tokens, st.n_tokens - shift)) new_ref = ref;
                 }
             }
             uint32_t x[4][32];
@@ -832,8 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
             }
             // Rows that stand for nothing, which hold anything, have no say in when the others' maxima move: their bits would depend on it.
             if (my_token >= min(slot_tokens, st.n_tokens - shift)) best = -INFINITY;
-            const int new_ref = st.ref;
-            if (__any_sync(0xffffffffu, best - m > kMaxLead) || new_ref != ref) {
+            if (__any_sync(0xffffffffu, best - m > kMaxLead || new_ref != ref)) {
                 if (!(ok = until_done())) break;
                 const float now = fmaxf(m, best), base = now == -INFINITY ? 0.f : now;
                 const float shrink = exp2_approx(m - base);  // 0 from -infinity on
@@ -974,7 +976,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_chunk_join_kernel(const 
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) sum += sum_of[w][lane];
     if (!valid) return;
-    const float inv = 1.f / sum, scale = __uint_as_float(static_cast<uint32_t>(127 + max(static_cast<int>(ref), -126)) << 23);
+    const float inv = 2.f / sum, scale = __uint_as_float(static_cast<uint32_t>(126 + max(static_cast<int>(ref), -125)) << 23);
     uint16_t *y = static_cast<uint16_t *>(const_cast<void *>(a.out.ptr)) + static_cast<int64_t>(unit.x + t) * a.out.token_stride + (unit.z + my_head) * a.out.head_stride;
     constexpr int kMine = D / 4 / kJoinWarps;
     float4 o[kMine];
