@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                         }
                     if (move_ref) {
                         float step = ref / sv_hi;
-                        if (sv_hi < ref_top * 0x1p-60f) {
+                        if (sv_hi < ref && sv_hi < ref_top * 0x1p-60f) {
                             // far below the largest r that O was summed with: r follows as long as O stays in range
                             float most = 0.f;
 #pragma unroll
