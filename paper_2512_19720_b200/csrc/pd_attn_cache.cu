@@ -303,6 +303,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
             for (int k = 0; k < 2; ++k) hidden[n][k] = CHUNK ? max(new_tokens - 1 - (n * 8 + 2 * t + k) / group, 0) : 0;
         uint32_t qf[KS][NT][3][2];
         float ref = 0.f, inv_ref = 0.f, ref_top = 0.f;  // the reference scale of V, its reciprocal, and the largest that O was summed with
+        float row_ref[NT][2];                           // the reference scale that a row's O is in, which pages that it does not attend to leave as it is
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 qs[n][k] = lscale * __shfl_sync(0xffffffffu, up + bad, (2 * t + k) * 4);
-                m[n][k] = -INFINITY, mu[n][k] = 0.f, l[n][k] = 0.f;
+                m[n][k] = -INFINITY, mu[n][k] = 0.f, l[n][k] = 0.f, row_ref[n][k] = 0.f;
             }
         }
 
@@ -448,6 +449,8 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                             m[n][k] = top, mu[n][k] = mu_new;
                         }
                     if (move_ref) {
+                        // a row that does not attend to the pages of this step attends to none behind them either
+                        auto follows = [&](int n, int k) { return !CHUNK || (sv[0] > 0.f && hidden[n][k] < left) || (sv[1] > 0.f && 16 + hidden[n][k] < left); };
                         float step = ref / sv_hi;
                         if (sv_hi < ref && sv_hi < ref_top * 0x1p-60f) {
                             // far below the largest r that O was summed with: r follows as long as O stays in range
@@ -458,7 +461,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                                     for (int k = 0; k < 4; ++k)
-                                        if (n * 8 + 2 * t + (k & 1) < rows) most = fmaxf(most, fabsf(o[j][n][k] * factor[n][k & 1]));
+                                        if (n * 8 + 2 * t + (k & 1) < rows && follows(n, k & 1)) most = fmaxf(most, fabsf(o[j][n][k] * factor[n][k & 1]));
 #pragma unroll
                             for (int d = 1; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
                             step = most > 0.f ? fmaxf(fminf(fminf(step, kMostOutput / most), 0x1p120f), 1.f) : 1.f;  // finite, however little is left of O
@@ -470,7 +473,10 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                         ref_top = fmaxf(ref_top, ref);
                         inv_ref = __frcp_rn(ref);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) factor[n][0] *= step, factor[n][1] *= step;
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+                                if (follows(n, k)) factor[n][k] *= step, row_ref[n][k] = ref;
                     }
 #pragma unroll
                     for (int j = 0; j < MT; ++j)
@@ -541,7 +547,7 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
                 const int r = n * 8 + 2 * t + k;
                 if (r < rows) {
                     if (whole) {
-                        const float f = l[n][k] == 0.f ? 0.f : ref / l[n][k];
+                        const float f = l[n][k] == 0.f ? 0.f : (CHUNK ? row_ref[n][k] : ref) / l[n][k];
                         uint32_t w[VB / 2];
 #pragma unroll
                         for (int j = 0; j < VB / 2; ++j) w[j] = E::from_float2(o[j][n][k] * f, o[j][n][k + 2] * f);
@@ -558,11 +564,12 @@ __global__ void __launch_bounds__(CacheShape<D, NT>::kThreads, 1) attn_cache_ker
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int r = n * 8 + 2 * t + k;
+                    const float unit = CHUNK ? row_ref[n][k] : ref;
                     if (r < rows) {
                         if (g == 0) pm[r] = m[n][k], pl[r] = l[n][k];
 #pragma unroll
                         for (int j = 0; j < VB / 2; ++j)
-                            *reinterpret_cast<float2 *>(po + r * D + VB * g + 2 * j) = make_float2(o[j][n][k] * kPart * ref, o[j][n][k + 2] * kPart * ref);
+                            *reinterpret_cast<float2 *>(po + r * D + VB * g + 2 * j) = make_float2(o[j][n][k] * kPart * unit, o[j][n][k + 2] * kPart * unit);
                     }
                 }
             if (lane == 0) pieces[warp][slot] = {first_unit, n_tiles, token0, head0, rows};

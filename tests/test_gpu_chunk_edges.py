@@ -102,7 +102,8 @@ def test_values_with_scales_at_the_ends_of_the_range(api, page, hq, hkv, d, new,
     assert bool(torch.isfinite(got.float()).all()) and not got[:new].any()
 
 
-@pytest.mark.parametrize("hq,hkv,d,page,new,most", [(4, 4, 64, 16, 120, 0), (4, 4, 128, 16, 300, 0), (8, 2, 64, 16, 30, 0), (40, 2, 128, 32, 40, 0), (1, 1, 128, 64, 200, 0)])
+@pytest.mark.parametrize("hq,hkv,d,page,new,most", [(4, 4, 64, 16, 120, 0), (4, 4, 128, 16, 300, 0), (8, 2, 64, 16, 30, 0), (40, 2, 128, 32, 40, 0), (1, 1, 128, 64, 200, 0),
+                                                    (4, 4, 64, 16, 16, 16), (8, 2, 128, 16, 4, 4), (3, 3, 64, 32, 5, 5), (4, 2, 128, 64, 8, 8)])
 @pytest.mark.parametrize("held,late", [(-5, 119), (-119, 120), (3, 40), (0, -119), (100, -119)])
 def test_later_pages_have_no_influence(api, held, late, hq, hkv, d, page, new, most):
     """Pages of later tokens whose values are larger or smaller by any factor do not change what earlier tokens see."""
@@ -119,7 +120,7 @@ def test_later_pages_have_no_influence(api, held, late, hq, hkv, d, page, new, m
         check_what_is_attended_to(api, pages, q, lens, [new, new], most, rows=rows)
 
 
-@pytest.mark.parametrize("hq,hkv,d,page,new,most", [(4, 4, 64, 16, 250, 0), (16, 2, 128, 16, 16, 0), (40, 2, 64, 32, 50, 0), (1, 1, 64, 16, 700, 0)])
+@pytest.mark.parametrize("hq,hkv,d,page,new,most", [(4, 4, 64, 16, 250, 0), (16, 2, 128, 16, 16, 0), (40, 2, 64, 32, 50, 0), (2, 2, 128, 16, 16, 16), (1, 1, 64, 16, 700, 0)])
 def test_every_token_sees_its_own_pages_only(api, hq, hkv, d, page, new, most):
     """Scales at random over the whole range, among the held tokens' pages too."""
     for seed in range(3):
