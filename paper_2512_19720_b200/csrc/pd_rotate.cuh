@@ -1,8 +1,9 @@
 // Rotary positions: angles and the rotation of 16 values, shared by the calls that rotate.
 //
-// The pair (x, y) of a head turns by t = position * frequency to (x cos t - y sin t, x sin t + y cos t).  The product is taken in 64
-// bits (positions and frequencies have 31 and 24) and brought to [-1/2, 1/2] turns there, so that far positions lose nothing: in 32
-// bits position 131071 at frequency 1 would be off by up to 2^-8 of a radian.
+// The pair (x, y) of a head turns by t = position * frequency to (x cos t - y sin t, x sin t + y cos t).  The product and its reduction to
+// [-1/2, 1/2] turns are done in 64 bits: in 32 bits the angle of position 131071 at a frequency next to 1 would be off by up to 2^-8 of a
+// radian.  Three roundings to 53 bits (the product, which has up to 55, the factor 1 / 2 pi and the product with it) leave an error below |t| 2^-51,
+// 2^-20 of a radian at the far end of the positions, and the rounding of the reduced angle to 32 bits one below 2^-23.
 #pragma once
 
 #include "pd_attn.cuh"

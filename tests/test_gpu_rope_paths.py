@@ -1,10 +1,10 @@
 """Paths of pd_kv_append_rope and pd_rope that only larger calls take: walks of a block over several heads, pages found by tokens, queries in
-a launch of their own.  Bounds are those of test_gpu_rope."""
+a launch of their own; and positions at the ends of their range.  Bounds are those of test_gpu_rope."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_rope import TYPES, check_append, check_turned, frequencies, i32, offsets
+from test_gpu_rope import SMALLEST, TURN, TYPES, UNIT, check_append, check_turned, f64, frequencies, i32, offsets, partner
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +72,30 @@ def test_many_queries(api, interleaved, given):
     again = q.clone()
     api.pd_kv_append_rope(again, k, v, *cache, cu, i32(lens), table, freq, positions if given else None, None, interleaved, q_out=again)
     assert torch.equal(again[first:last], turned[first:last]) and torch.equal(again[:first], q[:first]) and torch.equal(again[last:], q[last:])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_positions_at_the_ends_of_their_range(api, interleaved):
+    """The angle a = position * frequency is rounded to binary64 once, its part of a turn by the factor's and the product's rounding: below
+    2^-51 |a| in all, beside what test_gpu_rope counts.  The definition in 64-bit significands holds the product exactly."""
+    assert np.finfo(np.longdouble).nmant >= 63
+    places = [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 2, -2 ** 31 + 1, 2 ** 30 + 12345, -2 ** 30 - 54321, 1999999999, 131071, 2 ** 24 + 1, 0]
+    d, h = 64, 3
+    freq = frequencies(32)
+    freq[3], freq[5] = 0.9999999, 1.9999999
+    angles = np.array(places, dtype=np.longdouble)[:, None] * f64(freq).astype(np.longdouble)[None]
+    two_pi = np.longdouble("6.283185307179586476925286766559")
+    part = np.remainder(angles, two_pi).astype(np.float64)
+    for dtype in TYPES:
+        q = torch.randn(len(places), h, d, generator=torch.Generator("cuda").manual_seed(3), device="cuda").to(dtype)
+        x = f64(q)
+        a, b = (slice(0, 64, 2), slice(1, 64, 2)) if interleaved else (slice(0, 32), slice(32, 64))
+        loose = np.zeros_like(x)
+        loose[..., a] = loose[..., b] = np.abs(angles).astype(np.float64)[:, None] * 2.0 ** -51
+        for inverse in (False, True):
+            c, s = np.cos(part)[:, None], np.sin(part)[:, None] * (-1 if inverse else 1)
+            want = np.zeros_like(x)
+            want[..., a], want[..., b] = x[..., a] * c - x[..., b] * s, x[..., a] * s + x[..., b] * c
+            got, _ = api.pd_rope(q, None, i32(places), freq, None, interleaved, inverse)
+            bound = (UNIT[dtype] + 2.0 ** -30) * np.abs(want) + SMALLEST[dtype] + (TURN + loose) * partner(x, 32, interleaved)
+            assert np.all(np.abs(f64(got) - want) <= bound), float((np.abs(f64(got) - want) / bound).max())
