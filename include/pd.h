@@ -519,16 +519,21 @@ pd_status pd_kv_append_rope_bf16(const void *q, int64_t q_token_stride, int64_t 
  *
  *   q   : in,  [n_tokens, q_heads, head_dim], packed by cu_seqlens: the last cu_seqlens[b + 1] - cu_seqlens[b] tokens of sequence b,
  *         which has seq_lens[b] in all; none, one or many
- *   max_new : the most new tokens of a sequence, 0 for not known: where at most 16 pairs of a token and a query head share a key/value head,
- *         max_new * (q_heads / kv_heads), a call that says so is quicker
+ *   max_new : the most new tokens of a sequence, 0 for not known.  Where at most 16 pairs of a token and a query head share a key/value head,
+ *         max_new * (q_heads / kv_heads), a call that says so goes to pd_attn_cache's kernel.  Left out, every sequence pays for products of 128 rows: 64 single
+ *         tokens behind 4000, 64 heads on 8, take 221 us instead of 103
  *   out : out, [n_tokens, q_heads, head_dim]: token i of the n new ones attends to the cached tokens 0 .. seq_lens[b] - n + i
  * Rows of n_tokens that no sequence claims are left as they are.  Slots of a page behind what a token attends to and pages that it does not
- * reach have no influence on it, whatever they hold; a page whose scale is not finite makes the tokens that attend to any of it NaN.
+ * reach have no influence on it, whatever they hold, but for the last bits: neighbouring pages and the rows of a block share the powers of two that weights are rounded
+ * beside.  A page whose scale is not finite makes the tokens that attend to any of it NaN.
  * The cache holds fewer than 2^31 blocks of 16 tokens and one head (n_pages * kv_heads * page / 16).  Scores are any finite size; the sums of a query
  * times codes have to be finite in binary32 (magnitudes below 2^113).
- * Weights are rounded to binary16 (relative to the largest, times the scale of V's page, times 2^7) for their product with V; pages whose scale of V is below 2^-67 of the
- * largest of the sequence lose precision.  Offsets that decrease, more new tokens than max_new or than seq_lens[b] and lengths beyond the table
- * latch PD_ERR_BAD_INDEX, and the sequence is left out.  The same call gives the same bits.
+ * Weights are rounded to binary16 for their product with V: each is off by up to 2^-11 of itself, as much as a binary16 output is by its own rounding, and
+ * small ones by up to 2^-24 of the row's largest (2^-19 in pd_attn_cache's kernel).  The two kernels differ where scales of V are far apart.  pd_attn_cache's loses what is below 2^-100 of the values that
+ * have been summed; in the other one pages whose scale of V is below 2^-67 of the largest that the token attends to lose precision in the sum of the
+ * values, down to nothing, though not in that of the weights.
+ * Offsets that decrease, more new tokens than max_new or than seq_lens[b] and lengths beyond the table latch PD_ERR_BAD_INDEX, and the sequence is left
+ * out.  The same call gives the same bits.
  * Workspace: pd_workspace_bytes(PD_OP_ATTN_CHUNK, 0, 0, 0, 0) bytes (about 42 MB, for parts of rows whose keys are dealt to several blocks), of
  * which the first 131072 have to be zero before the first call.
  */

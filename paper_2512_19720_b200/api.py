@@ -608,7 +608,7 @@ def pd_kv_append_rope(q, k, v, k_codes, v_codes, k_scale, v_scale, cu_seqlens, s
 def pd_attn_chunk(q, k_codes, v_codes, k_scale, v_scale, cu_seqlens, seq_lens, block_table, max_new=0, scale=None, out=None, workspace=None):
     """Attention of the new tokens q [T, q_heads, head_dim] (packed by cu_seqlens; the last ones of each sequence of seq_lens[b] tokens) over the
     cache, which holds them already: each attends to itself and what is before it.  max_new: the most new tokens of a sequence, 0 for not
-    known.  Returns out [T, q_heads, head_dim]."""
+    known; steps of single or few tokens should give it, since without it they take about twice the time.  Returns out [T, q_heads, head_dim]."""
     dtype, index, shape = q.dtype, q.get_device(), q.shape
     view = _heads(q, "q", dtype, index)
     n_tokens, q_heads, head_dim = shape

@@ -5,6 +5,8 @@
 // passes it by more than 8.  Codes are exact in both 16-bit types, so that the products take them as they are: S = q C_k^T in the queries'
 // type, O = P C_v in binary16.  The scales go into the exponents.  With s_k, s_v the scales of a key's page and r a power of two,
 //     P = 2^(f s_k S - m + log2(s_v / r) + 7),   l = sum P r / s_v,   out = r O / l.
+// P is rounded to binary16, 2^-11 of a weight at most, what a binary16 output loses by its own rounding: the tensor cores take 16-bit weights, and a
+// second product with what is left of them would add 1024 of a tile's 2048 clocks of products.
 // r is a reference for the pages' scales of V: s_v / r is in [2^-7, 1], so that P stays normal in binary16 where the weight is above 2^-14.
 // Where a tile's pages differ by more than that it is gone through again for the others, the smallest first, which happens to hardly any cache.
 // Each row has an r of its own, which follows only where the row attends to a page that is taken: pages of later tokens, however large or
@@ -20,12 +22,13 @@
 // range ends inside a unit the parts are joined by a second kernel, in the order of the keys: results do not depend on the schedule.
 //
 // Bound.  By rows a tile of 128 keys is 2048 clocks of products and 2048 of the 16 exponentials a clock that an SM has, by keys the 32 KB of its
-// codes, 1370 clocks of the SM's share of the memory.  Measured: 2048 tokens behind 16384, 64 heads on 8: 1.28 ms, 0.91 PFLOP/s, 4700 clocks a
-// tile; 64 sequences of 4 tokens, 288 thousand keys (600 MB): 265 us, 4000 clocks a tile.  By rows the softmax's warps are busy all the time: half
+// codes, 1370 clocks of the SM's share of the memory.  Measured: 2048 tokens behind 16384, 64 heads on 8: 1.24 ms, 0.94 PFLOP/s, 4550 clocks a
+// tile; 64 sequences of 4 tokens, 288 thousand keys (600 MB): 262 us, 3950 clocks a tile.  By rows the softmax's warps are busy all the time: half
 // with the exponentials of both slots, half with the latencies of waits, loads and scales between them.  By keys it is the conversion: 16 KB
 // of codes take 900 to 1200 clocks, two of them a tile, with 300 clocks of waits each; its 64 KB of stores alone keep the shared memory busy
 // for 600.  Both suffer when the code of the 16 warps' roles does not fit into the SM's cache for instructions: the waits, loops and rings
-// are written for that (counters: warps that wait for instructions 1.2 -> 0.3 an issue, 1.33 -> 1.27 ms).
+// are written for that (counters: warps that wait for instructions 1.2 -> 0.3 an issue, 1.33 -> 1.27 ms;
+// one search for the reference of V's scales in the place of two: 1.29 -> 1.24 ms).
 // Tried and dropped: P in the place of the scores with both passes over them from tensor memory in loops (1.46 ms), two threads a row (2.5 ms: 24
 // warps), 8 warps for the conversion (no change), codes through registers instead of a ring in shared memory (1.75 ms, code too long).
 //

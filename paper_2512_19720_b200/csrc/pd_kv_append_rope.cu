@@ -23,8 +23,10 @@
 namespace pd {
 namespace {
 
-// Values of queries from which on they get a launch of their own, where more of them are under way: 9009 tokens with 64 heads of 128 88 us beside
-// 102; 2048 tokens with 32 heads 38 us beside 35, where the second launch's start costs more.
+// Values of queries from which on they get a launch of their own, where more of them are under way; below, the second launch's start costs more.
+// In a graph, 4 prompts, heads of 128, us with a launch of their own / without, at 0.5, 0.7, 1.0, 1.5 and 3.0 times the bound: 64 heads on 8
+// 23.2 / 22.1, 33.6 / 31.8, 43.2 / 43.8, 60.7 / 64.1, 107 / 119; 32 on 32 at 0.5, 0.75, 1.0 and 1.5: 59.9 / 56.1, 82.4 / 81.6, 105.6 / 105.5, 151 / 153; 32 on 8,
+// where the pages take less of the time, even at 0.5: 33.5 / 34.4, at 1.0 64.1 / 69.2.
 constexpr int64_t kManyQueries = 1 << 25;
 constexpr int kFew = 8;  // tokens: as many as two items a lane hold at head_dim 128
 
