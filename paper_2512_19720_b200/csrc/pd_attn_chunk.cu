@@ -758,10 +758,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunk_kernel(const __grid_co
                             for (int k = 0; k < 4; ++k) *reinterpret_cast<float4 *>(po + (c / 4 + k) * (256 * 4)) = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
                         }
                     }
-                    if (part >= 0 && valid) {
-                        const bool any = w0 != 0.f || w1 != 0.f;
-                        *reinterpret_cast<float4 *>(po + 256 * D) = make_float4(any ? m : -INFINITY, any ? sum : 0.f, static_cast<float>(at), 0.f);
-                    }
+                    // m and the sum count where nothing is left of O in this part's reference, too
+                    if (part >= 0 && valid) *reinterpret_cast<float4 *>(po + 256 * D) = make_float4(m, sum, static_cast<float>(at), 0.f);
                     tcgen05_fence_before();
                     __syncwarp();
                     if (lane == 0) {  // slot 1's barrier counts the warps of both slots, or its own ones twice

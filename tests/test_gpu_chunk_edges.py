@@ -159,3 +159,19 @@ def test_zeros_between_pages_of_very_different_scales(api, small, large, hq, hkv
         pages = with_scales([n, n + 128], hkv, d, page, [of_pages, [2.0 ** small] * 5 + of_pages[4:]], 43)
         q = queries(2 * new, hq, d, torch.bfloat16, 47)
         check_what_is_attended_to(api, pages, q, [n, n + 128], [new, new], rows=sorted({0, 1, new // 3, new // 2, new - 1}))
+
+
+@pytest.mark.parametrize("hq,hkv,d,new", [(6, 2, 64, 9), (40, 2, 128, 3), (4, 4, 64, 150)])
+@pytest.mark.parametrize("first", [2.0 ** -60, 0.0])
+def test_weights_count_in_parts_whose_values_vanish(api, first, hq, hkv, d, new):
+    """The first page has all the weight and tiny values or none, the others, up to 2^170 larger, hardly any: units of every length, cut anywhere."""
+    page = 64
+    for held in range(300, 2200, 173):
+        n = held + new
+        of_pages = [first, 0.0, 0.0] + [2.0 ** -32, 2.0 ** 110, 2.0 ** -30, 2.0 ** 79] * (n // page)
+        pages = with_scales([n, 3], hkv, d, page, [of_pages, [1.0]], 53)
+        pages.codes[0][..., 0] = -64
+        pages.codes[0][int(pages.table[0, 0]), ..., 0] = 64
+        q = 0.05 * queries(new + 2, hq, d, torch.float32, 59)
+        q[..., 0] = 150.0
+        check_what_is_attended_to(api, pages, q.bfloat16(), [n, 3], [new, 2], 0, 0.2, rows=sorted({0, new // 2, new - 1}))
