@@ -494,7 +494,8 @@ pd_status pd_rope_bf16(const void *q, int64_t q_token_stride, int64_t q_head_str
  *   q, q_out : queries, turned into q_out (which may be q itself) in the rows that a sequence claims; not looked at where q_heads is 0
  *   positions : NULL: a token turns with its place in its sequence, seq_lens[b] - (cu_seqlens[b + 1] - cu_seqlens[b]) for the first new one
  * Everything else as in pd_kv_append, with the turned keys in binary32 (they are not rounded to 16 bits before they are quantised) in the place
- * of k; k_values are the turned keys that the codes stand for.  Sequences with few new tokens and long pieces may be mixed freely.
+ * of k; k_values are the turned keys that the codes stand for.  Sequences with few new tokens and long pieces may be mixed freely.  Where offsets
+ * decrease, which is reported, pages of any of the call's sequences may be left unwritten.
  * Workspace: PD_OP_ATTN.
  */
 pd_status pd_kv_append_rope(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
